@@ -50,7 +50,7 @@ typedef enum {
   RT_ERR_TIMEOUT = 5        /* a bounded device-side wait expired; outputs are invalid */
 } rt_status;
 
-typedef enum { RT_F32 = 0, RT_BF16 = 1 } rt_dtype;
+typedef enum { RT_F32 = 0, RT_BF16 = 1, RT_E4M3 = 2 /* pages of an rt_paged_cache only */ } rt_dtype;
 
 /* RT_SCHED_TILED: Algorithm 1's schedule at leaf granularity (each K/V row is streamed
  * O(log N) times).  RT_SCHED_NAIVE: the token-sequential evaluation of Sec. 5 ("What makes
@@ -257,6 +257,102 @@ size_t    rt_backward_workspace_bytes(const rt_config *cfg, int32_t B, int32_t N
 rt_status rt_layer_backward(const rt_config *cfg, const rt_layer_weights *w, const void *x, const void *z, const float *dz,
                             int32_t B, int32_t N, float *dx, const rt_layer_grads *grads,
                             void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ---- caches in pages -----------------------------------------------------------------------
+ * The caches above are one array per layer in which all sequences have the same length.  A server whose sequences come
+ * and go at different lengths keeps their pairs in pages of a pool instead: page_size positions a page, a table that
+ * names the pages of every sequence, and optionally 8 bits a value.  (The paper has no counterpart: it times batches
+ * of one length.)  The operators below write such a cache, read it back, attend to it with one new token of every
+ * sequence, and make the queries and keys that go with it.  Shared heads (n_kv_heads < n_heads: query head h reads head
+ * h / (n_heads / n_kv_heads) of the cache) and heads of 64 or 128 dimensions.
+ *  - RT_E4M3 pages hold a row of a head (the head_dim keys or values of one position) as e4m3 codes times 2^k, where k
+ *    is the smallest integer >= -126 that brings the row's largest finite magnitude to at most 448; k + 127 is stored
+ *    in k_exp / v_exp.  Scaling by a power of two is exact, so the one rounding is that of x 2^-k to e4m3 (to nearest,
+ *    ties to even).  e4m3 has no infinity: infinities and NaN are stored as NaN.
+ *  - A negative position (rt_cache_write, rt_cache_read, rt_qk_rotate, its backward pass) or length (rt_paged_attention) marks
+ *    a row that is not in use: it is skipped and its outputs stay as they were.
+ *  - Sequence, position and page numbers are checked on the device.  Where one lies outside the table or the pool nothing is
+ *    read or written through it (rt_paged_attention: its pairs get no weight, and a length is cut to max_pages * page_size), and
+ *    *status becomes RT_ERR_INVALID_ARG.  No call ever clears that word: the caller zeroes it once and
+ *    reads it with rt_get_status.
+ *  - The entries of the page table behind a sequence's last page are never read, nor are positions behind its length.
+ *  - Strides are in elements, between the rows of consecutive tokens; a token's heads are contiguous.  Rows begin
+ *    at multiples of 16 bytes and do not overlap.  Index arrays and fp32 vectors (lens, lse, slopes) need 4-byte alignment only.
+ *  - The pointers belong to the device that is current. */
+typedef struct {
+  void *k, *v;                     /* pools [n_pages, n_kv_heads, page_size, head_dim] of `dtype` */
+  uint8_t *k_exp, *v_exp;          /* RT_E4M3: [n_pages, n_kv_heads, page_size]; NULL otherwise */
+  const int32_t *page_table;       /* [n_seqs, max_pages] page numbers; pages may be shared between sequences */
+  int32_t *status;                 /* one word, see above; NULL for none */
+  int32_t n_pages, page_size;      /* page_size: 16, 32, 64, 128 or 256 */
+  int32_t n_kv_heads, head_dim;    /* head_dim: 64 or 128 */
+  int32_t dtype;                   /* RT_F32, RT_BF16 or RT_E4M3 */
+  int32_t n_seqs, max_pages;
+} rt_paged_cache;
+
+/* Writes `rows` rows of keys and values, [rows, n_kv_heads, head_dim] of `dtype` (RT_F32 or RT_BF16), into their places:
+ * row r becomes position pos[r] of sequence seq[r] (device arrays).  Rounded once, to the cache's type.  Rows of one call
+ * name different places (a place that two rows name may end up with parts of both).
+ * rt_cache_read copies such rows out again, as the values they stand for, rounded once to `dtype`. */
+rt_status rt_cache_write(const rt_paged_cache *cache, int32_t dtype, const void *k, const void *v, int64_t k_stride,
+                         int64_t v_stride, const int32_t *seq, const int32_t *pos, int32_t rows, void *cuda_stream);
+rt_status rt_cache_read(const rt_paged_cache *cache, int32_t dtype, void *k, void *v, int64_t k_stride, int64_t v_stride,
+                        const int32_t *seq, const int32_t *pos, int32_t rows, void *cuda_stream);
+
+/* Attention of one new token of every sequence over its cached pairs j < lens[b] and, with k_own and v_own, over the token's
+ * own temporary pair (Sec. 2.2's attention of position i = lens[b]; without them the token's pair is the last cached
+ * one, as in an ordinary decoder):
+ *   a_j = softmax_scale <q, k_j> - alibi_slopes[h] (p - j),  p = lens[b] with an own pair (at distance 0), else lens[b] - 1
+ *   out = sum_j e^{a_j} v_j / sum_j e^{a_j},   lse = log sum_j e^{a_j}
+ * A sequence without any pair gets out = 0 and lse = -infinity.  All arithmetic is fp32 or as good (32-bit softmax statistics
+ * and sums, queries and weights to at least 2^-20); `out` is rounded once.  out must not overlap q.
+ * The work is split evenly over the GPU whatever the lengths are; the result does not depend on timing. */
+typedef struct {
+  const void *q;                   /* [n_seqs, n_heads, head_dim] of `dtype` */
+  const void *k_own, *v_own;       /* [n_seqs, n_kv_heads, head_dim] of `dtype`, or both NULL */
+  const int32_t *lens;             /* [n_seqs], device */
+  const float *alibi_slopes;       /* [n_heads] fp32, device, or NULL */
+  void *out;                       /* [n_seqs, n_heads, head_dim] of `dtype` */
+  float *lse;                      /* [n_seqs, n_heads], or NULL */
+  int64_t q_stride, k_own_stride, v_own_stride, out_stride;
+  int32_t dtype;                   /* RT_F32 or RT_BF16 */
+  int32_t n_heads;                 /* a multiple of n_kv_heads */
+  float softmax_scale;
+} rt_paged_query;
+size_t    rt_paged_attention_workspace_bytes(const rt_paged_cache *cache, int32_t n_heads);
+rt_status rt_paged_attention(const rt_paged_cache *cache, const rt_paged_query *query, void *workspace, size_t workspace_bytes,
+                             void *cuda_stream);
+
+/* qkRMS of queries and keys for each head (Sec. 2.2) and the rotation of pairs of dimensions by the position, in one pass:
+ *   y = x / sqrt(mean(x^2) + rms_eps) * g          (with norm_flags = RT_NORM_QK; otherwise y = x)
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),   t = pos[r] * freq[i],  i < rot_dim / 2
+ * with (a, b) = (i, i + rot_dim / 2) for RT_PAIRS_HALVES and (2 i, 2 i + 1) for RT_PAIRS_NEIGHBOURS; dimensions from rot_dim on are
+ * not rotated.  Angles are formed in 64 bits.  q_out may be q and k_out may be k (with the same stride). */
+enum { RT_PAIRS_HALVES = 0, RT_PAIRS_NEIGHBOURS = 1 };
+typedef struct {
+  int32_t dtype;                   /* RT_F32 or RT_BF16: queries, keys, gains and their outputs */
+  int32_t n_heads, n_kv_heads;     /* n_kv_heads = 0: queries only, the arguments of the keys are ignored */
+  int32_t head_dim;                /* 64 or 128 */
+  int32_t norm_flags;              /* RT_NORM_QK or 0 */
+  float rms_eps;
+  int32_t rot_dim;                 /* multiple of 16 from 0 to head_dim */
+  int32_t pairs;                   /* RT_PAIRS_* */
+  const double *freq;              /* HOST array of rot_dim / 2 angles per position (radians), read during the call */
+} rt_rotate_config;
+rt_status rt_qk_rotate(const rt_rotate_config *cfg, const void *q, const void *k, int64_t q_stride, int64_t k_stride,
+                       const void *g_q, const void *g_k, /* [heads * head_dim], NULL = ones */
+                       const int32_t *pos, int32_t rows, void *q_out, void *k_out, int64_t q_out_stride, int64_t k_out_stride,
+                       void *cuda_stream);
+
+/* Its backward pass: q, k, g_q, g_k, pos as given to rt_qk_rotate, dq_out = dL/dq_out [rows, n_heads, head_dim] and dk_out, fp32.
+ * Writes dq, dk (fp32; each may be the gradient that it is made from) and the gains' gradients dg_q, dg_k (fp32, [heads * head_dim],
+ * OVERWRITTEN, NULL = not wanted; zero without RT_NORM_QK).  A gain's rows are added up in a fixed order.
+ * All four gradient arrays are contiguous. */
+size_t    rt_qk_rotate_backward_workspace_bytes(const rt_rotate_config *cfg, int32_t rows);
+rt_status rt_qk_rotate_backward(const rt_rotate_config *cfg, const void *q, const void *k, int64_t q_stride, int64_t k_stride,
+                                const void *g_q, const void *g_k, const int32_t *pos, int32_t rows,
+                                const float *dq_out, const float *dk_out, float *dq, float *dk, float *dg_q, float *dg_k,
+                                void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* Self-test of the bounded device-side wait (no counterpart in the paper): enqueues a two-CTA kernel
  * whose grid barrier expects an arrival that never comes.  The wait gives up after its limit (2 s),

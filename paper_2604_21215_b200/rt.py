@@ -19,16 +19,18 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librt_b200.so")
 
 RT_OK, RT_ERR_INVALID_ARG, RT_ERR_UNSUPPORTED, RT_ERR_WORKSPACE, RT_ERR_CUDA, RT_ERR_TIMEOUT = range(6)
-RT_F32, RT_BF16 = 0, 1
+RT_F32, RT_BF16, RT_E4M3 = 0, 1, 2
 RT_SCHED_TILED, RT_SCHED_NAIVE = 0, 1
 RT_NORM_PRE, RT_NORM_QK, RT_NORM_SKIP_Z = 1, 2, 8
 RT_FLAG_BACKWARD_STEP_LAUNCHES = 1
+RT_PAIRS_HALVES, RT_PAIRS_NEIGHBOURS = 0, 1
 
 EXPORTS = ("rt_workspace_bytes", "rt_layer_prefill", "rt_stack_prefill", "rt_decode_step",
            "rt_layer_decode_step", "rt_get_status", "rt_status_string", "rt_plan_counters", "rt_plan_tiles",
            "rt_profile_enable", "rt_profile_read", "rt_layer_decode_step_static", "rt_update_tile", "rt_selftest_wait_expiry",
            "rt_recompute_workspace_bytes", "rt_layer_recompute", "rt_backward_workspace_bytes", "rt_layer_backward",
-           "rt_static_get_status")
+           "rt_static_get_status", "rt_cache_write", "rt_cache_read", "rt_paged_attention_workspace_bytes", "rt_paged_attention",
+           "rt_qk_rotate", "rt_qk_rotate_backward_workspace_bytes", "rt_qk_rotate_backward")
 RT_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -56,6 +58,23 @@ class RtCounters(C.Structure):
 
 class RtProfile(C.Structure):
     _fields_ = [("ms", C.c_double * 4), ("launches", C.c_uint64 * 4)]
+
+
+class RtPagedCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "page_table", "status")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "n_seqs", "max_pages")]
+
+
+class RtPagedQuery(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k_own", "v_own", "lens", "alibi_slopes", "out", "lse")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_own_stride", "v_own_stride", "out_stride")] + \
+               [("dtype", C.c_int32), ("n_heads", C.c_int32), ("softmax_scale", C.c_float)]
+
+
+class RtRotateConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("norm_flags", C.c_int32), ("rms_eps", C.c_float), ("rot_dim", C.c_int32), ("pairs", C.c_int32),
+                ("freq", C.POINTER(C.c_double))]
 
 
 PROFILE_CLASSES = ("prepass", "leaf", "tile", "other")
@@ -98,6 +117,19 @@ def _load():
     lib.rt_decode_step.restype = C.c_int
     lib.rt_decode_step.argtypes = [C.POINTER(RtConfig), I, C.POINTER(RtLayerWeights), P, P, I, P, I, I, P,
                                    C.POINTER(P), C.POINTER(P), I, P, Z, P]
+    L = C.c_int64
+    lib.rt_cache_write.restype = lib.rt_cache_read.restype = C.c_int
+    lib.rt_cache_write.argtypes = lib.rt_cache_read.argtypes = [C.POINTER(RtPagedCache), I, P, P, L, L, P, P, I, P]
+    lib.rt_paged_attention_workspace_bytes.restype = Z
+    lib.rt_paged_attention_workspace_bytes.argtypes = [C.POINTER(RtPagedCache), I]
+    lib.rt_paged_attention.restype = C.c_int
+    lib.rt_paged_attention.argtypes = [C.POINTER(RtPagedCache), C.POINTER(RtPagedQuery), P, Z, P]
+    lib.rt_qk_rotate.restype = C.c_int
+    lib.rt_qk_rotate.argtypes = [C.POINTER(RtRotateConfig), P, P, L, L, P, P, P, I, P, P, L, L, P]
+    lib.rt_qk_rotate_backward_workspace_bytes.restype = Z
+    lib.rt_qk_rotate_backward_workspace_bytes.argtypes = [C.POINTER(RtRotateConfig), I]
+    lib.rt_qk_rotate_backward.restype = C.c_int
+    lib.rt_qk_rotate_backward.argtypes = [C.POINTER(RtRotateConfig), P, P, L, L, P, P, P, I, P, P, P, P, P, P, P, Z, P]
     lib.rt_get_status.restype = C.c_int
     lib.rt_get_status.argtypes = [P]
     lib.rt_status_string.restype = C.c_char_p
@@ -193,6 +225,36 @@ def rt_layer_recompute(cfg, w, x, z_claim, B, N, z_out, k_cache, v_cache, N_max,
                                    workspace_bytes, stream)
 
 
+def rt_cache_write(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, stream) -> int:
+    return _lib.rt_cache_write(C.byref(cache), dtype, k, v, k_stride, v_stride, seq, pos, rows, stream)
+
+
+def rt_cache_read(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, stream) -> int:
+    return _lib.rt_cache_read(C.byref(cache), dtype, k, v, k_stride, v_stride, seq, pos, rows, stream)
+
+
+def rt_paged_attention_workspace_bytes(cache: RtPagedCache, n_heads: int) -> int:
+    return int(_lib.rt_paged_attention_workspace_bytes(C.byref(cache), n_heads))
+
+
+def rt_paged_attention(cache, query, workspace, workspace_bytes, stream) -> int:
+    return _lib.rt_paged_attention(C.byref(cache), C.byref(query), workspace, workspace_bytes, stream)
+
+
+def rt_qk_rotate(cfg, q, k, q_stride, k_stride, g_q, g_k, pos, rows, q_out, k_out, q_out_stride, k_out_stride, stream) -> int:
+    return _lib.rt_qk_rotate(C.byref(cfg), q, k, q_stride, k_stride, g_q, g_k, pos, rows, q_out, k_out, q_out_stride, k_out_stride, stream)
+
+
+def rt_qk_rotate_backward_workspace_bytes(cfg: RtRotateConfig, rows: int) -> int:
+    return int(_lib.rt_qk_rotate_backward_workspace_bytes(C.byref(cfg), rows))
+
+
+def rt_qk_rotate_backward(cfg, q, k, q_stride, k_stride, g_q, g_k, pos, rows, dq_out, dk_out, dq, dk, dg_q, dg_k, workspace, workspace_bytes,
+                          stream) -> int:
+    return _lib.rt_qk_rotate_backward(C.byref(cfg), q, k, q_stride, k_stride, g_q, g_k, pos, rows, dq_out, dk_out, dq, dk, dg_q, dg_k,
+                                      workspace, workspace_bytes, stream)
+
+
 def rt_selftest_wait_expiry(workspace, stream) -> int:
     return _lib.rt_selftest_wait_expiry(workspace, stream)
 
@@ -251,6 +313,32 @@ def _to_dev(a, dtype: str, device):
     if isinstance(a, np.ndarray):
         a = torch.from_numpy(np.ascontiguousarray(a))
     return a.to(device=device, dtype=_tdtype(dtype)).contiguous()
+
+
+def _require(ok: bool, where: str):
+    """What ctypes cannot see of a tensor (its device, type, shape, the order of its dimensions) is refused like a bad argument of the call."""
+    if not ok:
+        raise RtError(RT_ERR_INVALID_ARG, where)
+
+
+def _rows(t, heads: int, head_dim: int, n: int, dtype, device, where: str) -> tuple:
+    """(address, stride) of [n, heads, head_dim] or [n, heads * head_dim] rows whose heads are contiguous."""
+    _require(t.dtype == dtype and t.device == device and t.shape[0] == n and t.numel() == n * heads * head_dim, where)
+    st, sh = t.stride(), t.shape
+    if len(sh) == 3:
+        ok = sh[1] == heads and (st[2] == 1 or head_dim == 1) and (heads == 1 or st[1] == head_dim)
+    else:
+        ok = len(sh) == 2 and st[1] == 1
+    _require(ok or n == 0, where)
+    return t.data_ptr(), st[0]
+
+
+def _vector(t, n: int, dtype, device, where: str):
+    """Address of a contiguous array of n elements, None for None."""
+    if t is None:
+        return None
+    _require(t.dtype == dtype and t.device == device and t.numel() == n and t.is_contiguous(), where)
+    return t.data_ptr()
 
 
 _W_NAMES = ("w_q", "w_k", "w_v", "w_o", "w_up", "w_down")
@@ -491,3 +579,169 @@ class Stack:
         torch = _torch()
         f = lambda t: t[:N].permute(1, 0, 2).to(torch.float64).cpu().numpy()
         return [(f(k), f(v)) for k, v in zip(self.k_caches, self.v_caches)]
+
+
+class PagedCache:
+    """The pairs of one layer's sequences in pages, over tensors of the caller: k and v [n_pages, n_kv_heads, page_size, head_dim] (float32,
+    bfloat16 or float8_e4m3fn, the last with exponents k_exp and v_exp, uint8 [n_pages, n_kv_heads, page_size]) and page_table, int32
+    [n_seqs, max_pages].  Which pages a sequence owns is the caller's to say: it writes the page table.
+
+    The methods take device tensors, enqueue on the current stream and return; nothing is kept between calls but the status word."""
+
+    def __init__(self, k, v, page_table, k_exp=None, v_exp=None):
+        torch = _torch()
+        where = "PagedCache"
+        self.device, self.k, self.v, self.page_table, self.k_exp, self.v_exp = k.device, k, v, page_table, k_exp, v_exp
+        code = {torch.float32: RT_F32, torch.bfloat16: RT_BF16, torch.float8_e4m3fn: RT_E4M3}.get(k.dtype)
+        _require(k.is_cuda and code is not None and k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and v.device == k.device and
+                 k.is_contiguous() and v.is_contiguous(), where + ": k, v")
+        _require(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.device == k.device,
+                 where + ": page_table")
+        n_pages, n_kv, page, hd = k.shape
+        _require((k_exp is not None) == (code == RT_E4M3) and (v_exp is not None) == (code == RT_E4M3), where + ": exponents")
+        self._status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._c = RtPagedCache(k.data_ptr(), v.data_ptr(), _vector(k_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": k_exp"),
+                               _vector(v_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": v_exp"), page_table.data_ptr(),
+                               self._status.data_ptr(), n_pages, page, n_kv, hd, code, page_table.shape[0], page_table.shape[1])
+        self._codes = {torch.float32: RT_F32, torch.bfloat16: RT_BF16}
+        self._need: dict = {}                          # workspace bytes by number of query heads
+        _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, where + ": shape")
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, n_seqs: int, max_pages: int, head_dim: int = 64, dtype: str = "bf16",
+              device: str = "cuda:0"):
+        """A cache with pages of its own; every entry of its page table is -1 (no page)."""
+        torch = _torch()
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        t = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[dtype]
+        pool = lambda: torch.zeros(shape, dtype=torch.uint8, device=device).view(t) if dtype == "e4m3" else torch.zeros(shape, dtype=t, device=device)
+        exps = lambda: torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == "e4m3" else None
+        return cls(pool(), pool(), torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), exps(), exps())
+
+    def _stream(self) -> int:
+        return _torch().cuda.current_stream(self.device).cuda_stream
+
+    def write(self, k, v, seq, pos) -> None:
+        """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
+        seq[r] (int32); a negative position skips the row."""
+        torch, c, n = _torch(), self._c, k.shape[0]
+        where = "PagedCache.write"
+        _require(k.dtype in self._codes, where + ": k")
+        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": k")
+        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": v")
+        sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
+        with torch.cuda.device(self.device):
+            _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, self._stream()), "rt_cache_write")
+
+    def read(self, seq, pos, dtype: str = "bf16", k=None, v=None):
+        """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
+        Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
+        torch, c, n = _torch(), self._c, pos.shape[0]
+        where, t = "PagedCache.read", _tdtype(dtype)
+        shape = (n, c.n_kv_heads, c.head_dim)
+        k = torch.empty(shape, dtype=t, device=self.device) if k is None else k
+        v = torch.empty(shape, dtype=t, device=self.device) if v is None else v
+        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": k")
+        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": v")
+        sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
+        with torch.cuda.device(self.device):
+            _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, self._stream()), "rt_cache_read")
+        return k, v
+
+    def attend(self, q, lens, k_own=None, v_own=None, scale: Optional[float] = None, alibi_slopes=None, out=None, lse=None):
+        """One new token of every sequence: q [n_seqs, n_heads, head_dim] attends to its sequence's first lens[b] cached pairs (int32) and,
+        if given, to its own pair k_own, v_own [n_seqs, n_kv_heads, head_dim] -> out [n_seqs, n_heads, head_dim].  lse (float32
+        [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
+        whatever the memory holds)."""
+        torch, c = _torch(), self._c
+        where, B, hd = "PagedCache.attend", c.n_seqs, c.head_dim
+        _require(q.dtype in self._codes and q.dim() == 3, where + ": q")
+        H, t = q.shape[1], q.dtype
+        out = torch.empty((B, H, hd), dtype=t, device=self.device) if out is None else out
+        a = RtPagedQuery()
+        a.q, a.q_stride = _rows(q, H, hd, B, t, self.device, where + ": q")
+        a.out, a.out_stride = _rows(out, H, hd, B, t, self.device, where + ": out")
+        _require((k_own is None) == (v_own is None), where + ": k_own, v_own")
+        if k_own is not None:
+            a.k_own, a.k_own_stride = _rows(k_own, c.n_kv_heads, hd, B, t, self.device, where + ": k_own")
+            a.v_own, a.v_own_stride = _rows(v_own, c.n_kv_heads, hd, B, t, self.device, where + ": v_own")
+        a.lens = _vector(lens, B, torch.int32, self.device, where + ": lens")
+        a.alibi_slopes = _vector(alibi_slopes, H, torch.float32, self.device, where + ": alibi_slopes")
+        a.lse = _vector(lse, B * H, torch.float32, self.device, where + ": lse")
+        a.dtype, a.n_heads, a.softmax_scale = self._codes[t], H, 1.0 / math.sqrt(hd) if scale is None else scale
+        need = self._need.get(H)
+        if need is None:
+            need = self._need[H] = rt_paged_attention_workspace_bytes(c, H)
+            _require(need > 0, where + ": q")
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device)       # of its own for every call: calls on two streams may overlap
+        with torch.cuda.device(self.device):
+            _check(rt_paged_attention(c, a, ws.data_ptr(), need, self._stream()), "rt_paged_attention")
+        return out
+
+    def status(self) -> int:
+        """RT_OK, or RT_ERR_INVALID_ARG once a call met a sequence, position or page number that does not exist (after a synchronise)."""
+        with _torch().cuda.device(self.device):
+            return rt_get_status(self._status.data_ptr())
+
+
+class QkRotate:
+    """qkRMS of queries and keys for each head and the rotation by the position, for one layer's shapes.  The angle of pair i at position
+    p is p * freq[i], by default base^(-2 i / rot_dim).  The methods take device tensors and enqueue on the current stream."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, dtype: str = "bf16", head_dim: int = 64, rot_dim: Optional[int] = None,
+                 base: float = 10000.0, freq: Optional[Sequence[float]] = None, pairs: str = "halves", norm: bool = True,
+                 rms_eps: float = 1e-6):
+        self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = dtype, n_heads, n_kv_heads, head_dim
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        freq = [base ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)] if freq is None else list(freq)
+        _require(len(freq) == rot_dim // 2, "QkRotate: freq")
+        self._freq = (C.c_double * max(len(freq), 1))(*freq)
+        self.cfg = RtRotateConfig({"f32": RT_F32, "bf16": RT_BF16}[dtype], n_heads, n_kv_heads, head_dim, RT_NORM_QK if norm else 0, rms_eps,
+                                  rot_dim, {"halves": RT_PAIRS_HALVES, "neighbours": RT_PAIRS_NEIGHBOURS}[pairs], self._freq)
+        _require(rt_qk_rotate_backward_workspace_bytes(self.cfg, 1) > 0, "QkRotate: shape")
+
+    def _inputs(self, q, k, pos, g_q, g_k, where):
+        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], _tdtype(self.dtype), q.device
+        _require(q.is_cuda and (k is not None or self.n_kv_heads == 0), where + ": q, k")
+        qp, qs = _rows(q, self.n_heads, hd, n, t, dev, where + ": q")
+        kp, ks = _rows(k, self.n_kv_heads, hd, n, t, dev, where + ": k") if self.n_kv_heads else (None, 0)
+        return (n, t, dev, qp, qs, kp, ks, _vector(g_q, self.n_heads * hd, t, dev, where + ": g_q"),
+                _vector(g_k, self.n_kv_heads * hd, t, dev, where + ": g_k"), _vector(pos, n, torch.int32, dev, where + ": pos"))
+
+    def forward(self, q, k, pos, g_q=None, g_k=None, q_out=None, k_out=None):
+        """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
+        and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
+        torch = _torch()
+        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, "QkRotate.forward")
+        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=t, device=dev) if q_out is None else q_out
+        qo, qos = _rows(q_out, self.n_heads, self.head_dim, n, t, dev, "QkRotate.forward: q_out")
+        ko, kos = None, 0
+        if self.n_kv_heads:
+            k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=t, device=dev) if k_out is None else k_out
+            ko, kos = _rows(k_out, self.n_kv_heads, self.head_dim, n, t, dev, "QkRotate.forward: k_out")
+        with torch.cuda.device(dev):
+            _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, torch.cuda.current_stream(dev).cuda_stream),
+                   "rt_qk_rotate")
+        return q_out, k_out
+
+    def backward(self, q, k, pos, dq_out, dk_out, g_q=None, g_k=None, dq=None, dk=None):
+        """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
+        gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
+        torch = _torch()
+        where, f32, hd = "QkRotate.backward", _torch().float32, self.head_dim
+        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, where)
+        kn = n * self.n_kv_heads * hd
+        new = lambda heads: torch.empty((n, heads, hd), dtype=f32, device=dev)
+        dq = new(self.n_heads) if dq is None else dq
+        dk = (new(self.n_kv_heads) if dk is None else dk) if self.n_kv_heads else None
+        dgq = None if g_q is None else torch.empty(self.n_heads * hd, dtype=f32, device=dev)
+        dgk = None if g_k is None or not self.n_kv_heads else torch.empty(self.n_kv_heads * hd, dtype=f32, device=dev)
+        ptr = lambda x: None if x is None else x.data_ptr()
+        ws = torch.empty(rt_qk_rotate_backward_workspace_bytes(self.cfg, n), dtype=torch.uint8, device=dev)
+        with torch.cuda.device(dev):
+            _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, where + ": dq_out"),
+                                         _vector(dk_out, kn, f32, dev, where + ": dk_out") if kn else None,
+                                         _vector(dq, n * self.n_heads * hd, f32, dev, where + ": dq"),
+                                         _vector(dk, kn, f32, dev, where + ": dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
+                                         torch.cuda.current_stream(dev).cuda_stream), "rt_qk_rotate_backward")
+        return dq, dk, dgq, dgk
