@@ -1,169 +1,792 @@
 // Attention of one new token of every sequence over its cached pairs, in pages.
 //
-// A block owns a sequence, a head of the cache and up to four of the query heads that share it.  Its warps take the positions 32 at a
-// time; a row of keys or values lies on head_dim * size / 16 lanes, 16 bytes each, so a warp reads several positions' rows at once.  Every such
-// group of lanes keeps its own running maximum, sum and output (online softmax), and they are joined at the end.
+// Bound: HBM reads of the cached pairs (each is used once per head that shares it: one flop a byte for bf16, two for e4m3).
+//
+// Split.  The work of a call is a line of units: sequence by sequence, head of the cache by head, KT positions a unit.  Every warp of the
+// launch takes an equal piece of that line, wherever it begins and ends, so one long sequence among short ones costs no more than its bytes;
+// the pieces follow from the lengths alone, which each block adds up itself (no plan from the host, the lengths may change between
+// replays of a graph).  A warp writes the heads that it holds whole; of a head that it shares with other warps it leaves maximum, sum
+// and output in the workspace, and a second kernel joins them in the order of the positions (the result does not depend on timing).
+//
+// Stream.  Each warp runs its own ring of STAGES units in shared memory, filled by 16-byte asynchronous copies that run ahead over the ends of heads and
+// sequences.  Rows behind a length and pages that do not exist arrive as zeros, so what lies there never meets a product.
+//
+// Products.  One query row cannot fill a tensor-core tile, but a tile is the cheapest way to use a staged row for all heads that share it:
+// up to 8 query heads are rows 0-7 of the A operand of mma m16n8k16.  Rows 8-15 carry the second term of the same heads' fp32 numbers, split into 16-bit
+// terms; so scores and weights keep at least 22 bits.  Positions and dimensions are permuted so that each operand is one 16-byte load of a
+// row (an order of the contraction is free, and so is the order of the output's columns as long as the epilogue knows it): no transposition.
+//   bf16 pages: bf16 products, queries in 1 (bf16) or 3 terms (fp32), weights in 3 terms.
+//   e4m3 pages: codes are exact in fp16; fp16 products, queries (scaled by a power of two) in 1 or 2 terms, weights in 2 terms.  The keys' scales
+//   multiply the scores, the values' scales the weights, which are kept relative to the largest scaled weight so far (fp16's range).
+//   fp32 pages: CUDA cores, fp32 throughout.
+#include <cuda_fp16.h>
+
 #include "rt_paged.h"
 
 namespace rt {
 namespace {
 
-constexpr int kWarps = 8, kGroupMax = 4;
+constexpr int kWarps = 4, kRows = 8;      // warps of a block; query heads of a unit
+constexpr int kSms = 148;
+constexpr float kWeightScale = 1024.0f;   // fp16 weights lie in [0, 2^10]: their second term keeps 2^-35 of the largest
 
-// 16 bytes of a row -> floats
-__device__ __forceinline__ void unpack16(const uint4& a, float (&f)[4], float) {
-  f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+// ---- shapes ------------------------------------------------------------------------------------
+template <typename CT, int HD>
+struct Shape {
+  static constexpr int RB = HD * (int)sizeof(CT), NCH = RB / 16;             // bytes and 16-byte chunks of a row
+  static constexpr int KT = HD == 64 && sizeof(CT) < 4 ? 32 : 16;            // positions of a unit (16 of them lie in one page)
+  static constexpr int SUB = KT / 16;
+  static constexpr int KV = 2 * KT * RB;
+  static constexpr int EXP = sizeof(CT) == 1 ? 2 * KT : 0;
+  static constexpr int STAGE = (KV + EXP + 16 + 127) / 128 * 128 < kRows * (HD + 2) * 4 ? (kRows * (HD + 2) * 4 + 127) / 128 * 128
+                                                                                         : (KV + EXP + 16 + 127) / 128 * 128;
+  static constexpr int STAGES = KV <= 4096 ? 4 : 3;
+  static constexpr int CTAS = KV <= 4096 ? 3 : KV <= 8192 ? 2 : 1;           // blocks of an SM (shared memory)
+  static constexpr int SMEM = kWarps * STAGES * STAGE;
+  static constexpr int WORKERS = kSms * CTAS * kWarps;
+};
+
+// ---- the line of units -------------------------------------------------------------------------
+struct Line {
+  int per;              // sequences per thread of the scan
+  long long total;
+};
+
+template <int KT>
+__device__ __forceinline__ int clamp_len(const PagedAttnParams& p, int b) {
+  const int n = __ldg(p.q.lens + b);
+  const long long room = (long long)p.c.max_pages << p.log_page;
+  return n > room ? (int)room : n;
 }
-__device__ __forceinline__ void unpack16(const uint4& a, float (&f)[8], __nv_bfloat16) { unpack8(a, f); }
-__device__ __forceinline__ void unpack16(const uint4& a, float (&f)[16], __nv_fp8_e4m3) {
-  const unsigned w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 t = from_e4m3x2(w[i / 2] >> (i % 2 * 16));
-    f[2 * i] = t.x; f[2 * i + 1] = t.y;
+template <int KT>
+__device__ __forceinline__ int tiles_of(int n) { return n < 0 ? 0 : max(1, (n + KT - 1) / KT); }
+
+// Units before each thread's first sequence, in sum[] (THREADS entries), and the total.  All threads of the block call.
+template <int KT, int THREADS>
+__device__ __forceinline__ Line scan_line(const PagedAttnParams& p, int items, long long* sum, long long* warp_sums, bool report) {
+  Line ln;
+  ln.per = (p.c.n_seqs + THREADS - 1) / THREADS;
+  const int b0 = threadIdx.x * ln.per;
+  long long mine = 0;
+  const long long room = (long long)p.c.max_pages << p.log_page;
+  for (int b = b0; b < min(b0 + ln.per, p.c.n_seqs); ++b) {
+    const int n = __ldg(p.q.lens + b);
+    if (report && n > room && p.c.status) *p.c.status = RT_ERR_INVALID_ARG;
+    mine += (long long)tiles_of<KT>(clamp_len<KT>(p, b)) * items;
   }
+  long long inc = mine;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long t = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += t;
+  }
+  if (lane == 31) warp_sums[warp] = inc;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < warp) before += warp_sums[w];
+    total += warp_sums[w];
+  }
+  sum[threadIdx.x] = before + inc - mine;
+  __syncthreads();
+  ln.total = total;
+  return ln;
 }
 
-__device__ __forceinline__ float q_at(const rt_paged_query& q, const void* p, size_t i) {
-  return q.dtype == RT_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : ((const float*)p)[i];
+// how many warps share the line, and which one holds a unit
+__device__ __forceinline__ long long workers_of(long long total, int workers) { return total < workers ? total : workers; }
+__device__ __forceinline__ long long worker_of(long long u, long long total, long long w) { return ((u + 1) * w - 1) / total; }
+
+struct Cursor { int b, item, tile, tiles, n; };      // item = head of the cache * slices + slice of its query heads
+
+template <int KT>
+__device__ __forceinline__ void next_unit(const PagedAttnParams& p, int items, Cursor& c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.item < items) return;
+  c.item = 0;
+  do {
+    if (++c.b >= p.c.n_seqs) { c.b = p.c.n_seqs - 1; return; }               // (behind the line's end: never used)
+    c.n = clamp_len<KT>(p, c.b);
+  } while (c.n < 0);
+  c.tiles = tiles_of<KT>(c.n);
 }
 
-template <typename CT, int HD, int G>
-__global__ void __launch_bounds__(kWarps * 32) paged_attn_kernel(const __grid_constant__ PagedAttnParams p) {
-  constexpr int E = 16 / sizeof(CT), LPK = HD / E, KPI = 32 / LPK;
-  __shared__ float sm_o[kWarps][G][HD], sm_m[kWarps][G], sm_l[kWarps][G];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / LPK, c = lane % LPK;
-  const int b = blockIdx.x / p.c.n_kv_heads, kvh = blockIdx.x % p.c.n_kv_heads;
-  const int h0 = kvh * p.group + blockIdx.y * G, g_in = min(G, p.group - blockIdx.y * G);
-  int n = __ldg(p.q.lens + b);
-  if (n < 0) return;
-  const long long room = (long long)p.c.max_pages * p.c.page_size;
-  if (n > room) {
-    if (threadIdx.x == 0 && p.c.status) *p.c.status = RT_ERR_INVALID_ARG;
-    n = (int)room;
-  }
-  const int at = p.q.k_own ? n : n - 1;                            // the query's position
-  float q[G][E], slope[G], m[G], l[G], o[G][E];
+// ---- small pieces ------------------------------------------------------------------------------
+__device__ __forceinline__ float q_at(int dtype, const void* p, size_t i) {
+  return dtype == RT_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : ((const float*)p)[i];
+}
+__device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {      // bytes = 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes));
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ unsigned pack_h2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&h);
+}
+// (a, b) rounded to 16-bit types, and what the rounding left
+__device__ __forceinline__ unsigned take_bf16(float& a, float& b) {
+  const unsigned w = pack2(a, b);
+  a -= __uint_as_float(w << 16); b -= __uint_as_float(w & 0xffff0000u);
+  return w;
+}
+__device__ __forceinline__ unsigned take_f16(float& a, float& b) {
+  const unsigned w = pack_h2(a, b);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  a -= f.x; b -= f.y;
+  return w;
+}
+__device__ __forceinline__ unsigned e4m3x2_to_h2(unsigned v) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v & 0xffffu), __NV_E4M3);
+  return *reinterpret_cast<const unsigned*>(&h);
+}
+
+// Places of 16-byte chunks in a staged tile of 16 rows, such that neither the copies nor the loads below meet bank conflicts: keys are read by
+// (row r, chunk c mod 4) with two rows at a time, values by (rows 0, 2, 4, 6, neighbouring chunks).
+template <int NCH> __device__ __forceinline__ int key_place(int row, int ch) { return NCH >= 8 ? row * NCH + (ch ^ ((row & 1) << 2)) : row * NCH + ch; }
+template <int NCH> __device__ __forceinline__ int value_place(int row, int ch) {
+  const int x = ((row >> 1) & 3) << 1;
+  return NCH >= 8 ? row * NCH + (ch ^ x) : (row >> 1) * 8 + ((((row & 1) << 2) + ch) ^ x);
+}
+
+// ---- tensor-core consumer ------------------------------------------------------------------------
+// Lane (r = lane / 4, c = lane % 4) holds row (query head) r of scores and outputs: positions 8 t + 2 c + {0, 1} of score tile t, and DL = HD / 4
+// dimensions from DL' * c on (see dim()).
+template <typename CT, int HD, bool QF32>
+struct Mma {
+  using S = Shape<CT, HD>;
+  static constexpr bool F8 = sizeof(CT) == 1;
+  static constexpr int KS = HD / 16, NT = S::KT / 8, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
+  unsigned q[TERMS][KS][2];
+  float o[HD / 8][4];
+  float m, l, mv, q_scale;                 // running maximum (log2 units), this lane's part of the sum, maximum of the scaled weights (F8)
+  float slope;
+
+  // Where a product of weights and values adds up.  The tensor core cuts what a sum loses instead of rounding it, which over thousands of
+  // positions would show in an fp32 output (up to n / 16 half steps): there the products of 16 positions are added with ordinary sums.
+  struct Out {
+    float c[4];
+    __device__ __forceinline__ Out(const float (&o)[4]) {
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int h = h0 + min(g, g_in - 1);
-    slope[g] = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h) * kLog2e : 0.f;
-    m[g] = -INFINITY; l[g] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) { q[g][e] = q_at(p.q, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + c * E + e); o[g][e] = 0.f; }
-  }
-  for (int j0 = warp * KPI; j0 < n; j0 += kWarps * KPI) {
-    const int j = j0 + sub;
-    int page = -1;
-    if (j < n) page = page_at(p.c, b, j >> p.log_page);
-    const bool ok = page >= 0;
-    float kf[E], vf[E], ks = 1.f, vs = 1.f;
-    const size_t row = ((size_t)(ok ? page : 0) * p.c.n_kv_heads + kvh) * p.c.page_size + (size_t)(j & (p.c.page_size - 1));
-    uint4 kr = make_uint4(0, 0, 0, 0), vr = kr;
-    if (ok) {
-      kr = __ldg((const uint4*)p.c.k + row * LPK + c);
-      vr = __ldg((const uint4*)p.c.v + row * LPK + c);
-      if (sizeof(CT) == 1) { ks = scale_of(__ldg(p.c.k_exp + row)); vs = scale_of(__ldg(p.c.v_exp + row)); }
+      for (int e = 0; e < 4; ++e) c[e] = QF32 ? 0.f : o[e];
     }
-    unpack16(kr, kf, CT());
-    unpack16(vr, vf, CT());
+    __device__ __forceinline__ void add(float (&o)[4]) const {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = QF32 ? o[e] + c[e] : c[e];
+    }
+  };
+
+  __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in, int lane) {
+    const int r = lane >> 2, c = lane & 3;
+    const bool in = r < g_in;
+    const size_t at = (size_t)b * p.q.q_stride + (size_t)(h0 + (in ? r : 0)) * HD;
+    float x[HD / 4];
+#pragma unroll
+    for (int i = 0; i < S::NCH / 4; ++i) {
+#pragma unroll
+      for (int e = 0; e < E; e += 8) {
+        float f[8];
+        const size_t d = at + (size_t)(c + 4 * i) * E + e;
+        if (p.q.dtype == RT_BF16) load8((const __nv_bfloat16*)p.q.q + d, f);
+        else load8((const float*)p.q.q + d, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[i * E + e + k] = in ? f[k] : 0.f;
+      }
+    }
+    q_scale = p.scale_log2;
+    if (F8) {                              // the largest of the row to [2^10, 2^11)
+      float a = 0.f;
+#pragma unroll
+      for (int d = 0; d < HD / 4; ++d) a = fmaxf(a, fabsf(x[d]));
+      a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+      a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+      const int k = min(137 - (int)(__float_as_uint(a) >> 23), 100);       // 10 - floor(log2 a), at least -118
+      const float up = __uint_as_float((unsigned)(127 + k) << 23);
+#pragma unroll
+      for (int d = 0; d < HD / 4; ++d) x[d] *= up;
+      q_scale *= __uint_as_float((unsigned)(127 - k) << 23);
+    }
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        q[t][s][0] = F8 ? take_f16(x[4 * s], x[4 * s + 1]) : take_bf16(x[4 * s], x[4 * s + 1]);
+        q[t][s][1] = F8 ? take_f16(x[4 * s + 2], x[4 * s + 3]) : take_bf16(x[4 * s + 2], x[4 * s + 3]);
+      }
+    slope = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h0 + (in ? r : 0)) * kLog2e : 0.f;
+    m = mv = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+  }
+
+  // one staged unit: positions j0 .. j0 + KT, of which live[s] of the s-th sixteen count; the query is at position `at`
+  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, const int (&live)[S::SUB], int lane) {
+    const int r = lane >> 2, c = lane & 3;
+    float s[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+      const uint4* kt = reinterpret_cast<const uint4*>(st + (t / 2) * 16 * S::RB);
+      const int row = (t & 1) * 8 + r;
+#pragma unroll
+      for (int i = 0; i < S::NCH / 4; ++i) {
+        const uint4 w = kt[key_place<S::NCH>(row, c + 4 * i)];
+        const unsigned x[4] = {w.x, w.y, w.z, w.w};
+        constexpr int KC = E / 4;          // contraction steps of a chunk
+#pragma unroll
+        for (int u = 0; u < KC; ++u) {
+          const int k = i * KC + u;
+          unsigned b0, b1;
+          if (F8) { b0 = e4m3x2_to_h2(x[u]); b1 = e4m3x2_to_h2(x[u] >> 16); }
+          else { b0 = x[2 * u]; b1 = x[2 * u + 1]; }
+          const unsigned z = 0u;
+          if (F8) mma_f16(s[t], q[0][k][0], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][0] : z, q[0][k][1], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][1] : z, b0, b1);
+          else {
+            mma_bf16(s[t], q[0][k][0], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][0] : z, q[0][k][1], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][1] : z, b0, b1);
+            if (TERMS > 2) mma_bf16(s[t], q[TERMS - 1][k][0], z, q[TERMS - 1][k][1], z, b0, b1);
+          }
+        }
+      }
+    }
+    // scores in log2 units, the maximum of the row, weights
+    const uint8_t* ke = st + S::KV;
+    const uint8_t* ve = ke + S::KT;
+    float a[NT][2], vs[NT][2], top = m, topv = mv;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      unsigned kx = 0, vx = 0;
+      if (F8) {
+        kx = *reinterpret_cast<const uint16_t*>(ke + 8 * t + 2 * c);
+        vx = *reinterpret_cast<const uint16_t*>(ve + 8 * t + 2 * c);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = TERMS > 1 ? s[t][e] + s[t][e + 2] : s[t][e];
+        x *= q_scale;
+        const int j = 8 * t + 2 * c + e;
+        const unsigned kb = (kx >> (8 * e)) & 0xffu, vb = (vx >> (8 * e)) & 0xffu;
+        if (F8) x *= scale_of(kb);
+        x -= slope * (float)(at - j0 - j);
+        a[t][e] = (j & 15) < live[t / 2] ? x : -INFINITY;
+        top = fmaxf(top, a[t][e]);
+        if (F8) {
+          vs[t][e] = scale_of(vb);
+          topv = fmaxf(topv, a[t][e] + (float)((int)vb - 127));
+        }
+      }
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if (F8) {
+      topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, 1));
+      topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, 2));
+    }
+    if (__any_sync(0xffffffffu, top > m || (F8 && topv > mv))) {
+      const float w = m == -INFINITY ? 0.f : exp2f(m - top);
+      const float wo = F8 ? (mv == -INFINITY ? 0.f : exp2f(mv - topv)) : w;
+      l *= w;
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] *= wo;
+      m = top;
+      mv = topv;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    const float to16 = !F8 ? 1.f : mv == -INFINITY ? 0.f : kWeightScale * exp2f(m - mv);
+#pragma unroll
+    for (int sub = 0; sub < S::SUB; ++sub) {
+      float w[4];                          // positions 2c, 2c + 1, 8 + 2c, 9 + 2c of the sixteen
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int t = 2 * sub + e / 2;
+        w[e] = exp2f(a[t][e & 1] - ref);
+        l += w[e];
+        if (F8) w[e] = w[e] * vs[t][e & 1] * to16;
+      }
+      unsigned w0[2], w1[2], w2[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (F8) { w0[h] = take_f16(w[2 * h], w[2 * h + 1]); w1[h] = take_f16(w[2 * h], w[2 * h + 1]); w2[h] = 0; }
+        else {
+          w0[h] = take_bf16(w[2 * h], w[2 * h + 1]); w1[h] = take_bf16(w[2 * h], w[2 * h + 1]);
+          w2[h] = pack2(w[2 * h], w[2 * h + 1]);
+        }
+      }
+      const unsigned char* vt = st + S::KT * S::RB + sub * 16 * S::RB;
+      const int rows[4] = {2 * c, 2 * c + 1, 8 + 2 * c, 9 + 2 * c};
+      if (!F8) {
+#pragma unroll
+        for (int i = 0; i < S::NCH / 8; ++i) {         // chunk r + 8 i of the four rows: dimensions 64 i + 8 r + (0 .. 7)
+          unsigned x[4][4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH>(rows[k], r + 8 * i)];
+            x[k][0] = y.x; x[k][1] = y.y; x[k][2] = y.z; x[k][3] = y.w;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
+            const unsigned b0 = __byte_perm(x[0][j / 2], x[1][j / 2], sel), b1 = __byte_perm(x[2][j / 2], x[3][j / 2], sel);
+            Out acc(o[8 * i + j]);
+            mma_bf16(acc.c, w0[0], w1[0], w0[1], w1[1], b0, b1);
+            mma_bf16(acc.c, w2[0], 0u, w2[1], 0u, b0, b1);
+            acc.add(o[8 * i + j]);
+          }
+        }
+      } else {
+        constexpr int WD = HD / 32;                    // words of this lane: dimensions 4 WD r + (0 .. 4 WD)
+        unsigned x[4][WD];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (WD == 2) {
+            const uint2 y = *reinterpret_cast<const uint2*>(vt + value_place<S::NCH>(rows[k], r >> 1) * 16 + (r & 1) * 8);
+            x[k][0] = y.x; x[k][1] = y.y;
+          } else {
+            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH>(rows[k], r)];
+            x[k][0] = y.x; x[k][1] = y.y; x[k][2] = y.z; x[k][3] = y.w;
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < WD; ++d) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const unsigned sel = h ? 0x7362u : 0x5140u;
+            const unsigned y0 = __byte_perm(x[0][d], x[1][d], sel), y1 = __byte_perm(x[2][d], x[3][d], sel);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float (&to)[4] = o[4 * d + 2 * h + e];
+              Out acc(to);
+              mma_f16(acc.c, w0[0], w1[0], w0[1], w1[1], e4m3x2_to_h2(y0 >> (16 * e)), e4m3x2_to_h2(y1 >> (16 * e)));
+              acc.add(to);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // Maximum, sum and output of every row into shared memory: out[r][HD], ml[r][2].  False if a row of the first g_in is not finite.
+  __device__ __forceinline__ bool dump(float* out, int g_in, int lane) {
+    const int r = lane >> 2, c = lane & 3;
+    float all = 0.f;
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    const float back = F8 ? (mv == -INFINITY ? 0.f : exp2f(mv - m) * (1.f / kWeightScale)) : 1.f;
+#pragma unroll
+    for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        // column 2 c + e of output tile j
+        const int d = F8 ? (HD / 8) * (2 * c + e) + j : (j / 8) * 64 + 8 * (2 * c + e) + j % 8;
+        const float y = (o[j][e] + o[j][e + 2]) * back;
+        out[r * HD + d] = y;
+        all = fmaf(y, 0.f, all);           // NaN once one is not finite
+      }
+    if (c == 0) { out[kRows * HD + 2 * r] = m; out[kRows * HD + 2 * r + 1] = l; }
+    return !__any_sync(0xffffffffu, r < g_in && !(all == 0.f && l < INFINITY));
+  }
+};
+
+// ---- fp32 pages: CUDA cores ----------------------------------------------------------------------
+// HD / 4 lanes a row, 128 / HD rows at a time; every such group of lanes has its own running maximum, sum and output, joined at the end.
+template <int HD, int G>
+struct Simt {
+  using S = Shape<float, HD>;
+  static constexpr int LPK = HD / 4, KPI = 32 / LPK;
+  float q[G][4], o[G][4], m[G], l[G], slope[G];
+  int g_in;
+
+  __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in_, int lane) {
+    g_in = g_in_;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      float a = 0.f;
+      const int h = h0 + min(g, g_in - 1);
+      slope[g] = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h) * kLog2e : 0.f;
+      m[g] = -INFINITY; l[g] = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) a += q[g][e] * kf[e];
-#pragma unroll
-      for (int w = LPK / 2; w; w >>= 1) a += __shfl_xor_sync(0xffffffffu, a, w);
-      a = ok ? a * ks * p.scale_log2 - slope[g] * (float)(at - j) : -INFINITY;
-      const float mn = fmaxf(m[g], a), ref = mn == -INFINITY ? 0.f : mn;
-      const float w0 = exp2f(m[g] - ref), w1 = exp2f(a - ref), wv = w1 * vs;
-      m[g] = mn;
-      l[g] = l[g] * w0 + w1;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[g][e] = o[g][e] * w0 + (ok ? wv * vf[e] : 0.f);
+      for (int e = 0; e < 4; ++e) {
+        q[g][e] = q_at(p.q.dtype, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + (lane % LPK) * 4 + e);
+        o[g][e] = 0.f;
+      }
     }
   }
-  // the lane groups of a warp, then the warps
+  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, const int (&live)[S::SUB], int lane) {
+    const int sub = lane / LPK, c = lane % LPK;
+#pragma unroll 4
+    for (int i = 0; i < 16 / KPI; ++i) {
+      const int j = i * KPI + sub;
+      const bool ok = j < live[0];
+      const float4 k = reinterpret_cast<const float4*>(st)[key_place<S::NCH>(j, c)];
+      const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH>(j, c)];
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
+      for (int g = 0; g < G; ++g) {
+        float a = q[g][0] * k.x + q[g][1] * k.y + q[g][2] * k.z + q[g][3] * k.w;
 #pragma unroll
-    for (int w = LPK; w < 32; w <<= 1) {
-      const float mo = __shfl_xor_sync(0xffffffffu, m[g], w), lo = __shfl_xor_sync(0xffffffffu, l[g], w);
-      const float mn = fmaxf(m[g], mo), ref = mn == -INFINITY ? 0.f : mn;
-      const float w0 = exp2f(m[g] - ref), w1 = exp2f(mo - ref);
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[g][e] = o[g][e] * w0 + __shfl_xor_sync(0xffffffffu, o[g][e], w) * w1;
-      l[g] = l[g] * w0 + lo * w1;
-      m[g] = mn;
-    }
-    if (sub == 0) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) sm_o[warp][g][c * E + e] = o[g][e];
-      if (c == 0) { sm_m[warp][g] = m[g]; sm_l[warp][g] = l[g]; }
+        for (int w = LPK / 2; w; w >>= 1) a += __shfl_xor_sync(0xffffffffu, a, w);
+        a = ok ? a * p.scale_log2 - slope[g] * (float)(at - j0 - j) : -INFINITY;
+        const float mn = fmaxf(m[g], a), ref = mn == -INFINITY ? 0.f : mn;
+        const float w0 = exp2f(m[g] - ref), w1 = exp2f(a - ref);
+        m[g] = mn;
+        l[g] = l[g] * w0 + w1;
+        o[g][0] = o[g][0] * w0 + w1 * v.x; o[g][1] = o[g][1] * w0 + w1 * v.y;      // (rows that do not count are zeros)
+        o[g][2] = o[g][2] * w0 + w1 * v.z; o[g][3] = o[g][3] * w0 + w1 * v.w;
+      }
     }
   }
-  __syncthreads();
-  constexpr int D = HD / 32;
-  for (int g = warp; g < g_in; g += kWarps) {
+  __device__ __forceinline__ bool dump(float* out, int, int lane) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+#pragma unroll
+      for (int w = LPK; w < 32; w <<= 1) {
+        const float mo = __shfl_xor_sync(0xffffffffu, m[g], w), lo = __shfl_xor_sync(0xffffffffu, l[g], w);
+        const float mn = fmaxf(m[g], mo), ref = mn == -INFINITY ? 0.f : mn;
+        const float w0 = exp2f(m[g] - ref), w1 = exp2f(mo - ref);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[g][e] = o[g][e] * w0 + __shfl_xor_sync(0xffffffffu, o[g][e], w) * w1;
+        l[g] = l[g] * w0 + lo * w1;
+        m[g] = mn;
+      }
+      if (lane < LPK && g < g_in) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[g * HD + lane * 4 + e] = o[g][e];
+        if (lane == 0) { out[kRows * HD + 2 * g] = m[g]; out[kRows * HD + 2 * g + 1] = l[g]; }
+      }
+    }
+    return true;
+  }
+};
+
+// What Mma::dump leaves, position by position from the pages, for heads whose result is not finite: the terms of a split number meet an
+// infinity with either sign, or as zeros, so an infinite key or value that counts would come out as NaN.
+template <typename CT, int HD>
+__device__ __noinline__ void slow_piece(const PagedAttnParams& p, int b, int kvh, int h0, int g_in, int j0, int j1, int at, float* out, int lane) {
+  for (int g = 0; g < g_in; ++g) {
     const int h = h0 + g;
-    float ma = -INFINITY, own = -INFINITY;
+    const float slope = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h) * kLog2e : 0.f;
+    float q[HD / 32], o[HD / 32], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) ma = fmaxf(ma, sm_m[w][g]);
-    if (p.q.k_own) {
+    for (int d = 0; d < HD / 32; ++d) { q[d] = q_at(p.q.dtype, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + d * 32 + lane); o[d] = 0.f; }
+    for (int j = j0; j < j1; ++j) {
+      const int page = __ldg(p.c.page_table + (size_t)b * p.c.max_pages + (j >> p.log_page));
+      if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
+      const size_t row = ((size_t)page * p.c.n_kv_heads + kvh) * p.c.page_size + (j & (p.c.page_size - 1));
+      const CT *k = (const CT*)p.c.k + row * HD, *v = (const CT*)p.c.v + row * HD;
+      const float ks = sizeof(CT) == 1 ? scale_of(p.c.k_exp[row]) : 1.f, vs = sizeof(CT) == 1 ? scale_of(p.c.v_exp[row]) : 1.f;
       float a = 0.f;
 #pragma unroll
-      for (int d = 0; d < D; ++d)
-        a += q_at(p.q, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + d * 32 + lane) *
-             q_at(p.q, p.q.k_own, (size_t)b * p.q.k_own_stride + (size_t)kvh * HD + d * 32 + lane);
-      own = warp_sum(a) * p.scale_log2;
-      ma = fmaxf(ma, own);
-    }
-    const float ref = ma == -INFINITY ? 0.f : ma;
-    float la = 0.f, oa[D];
+      for (int d = 0; d < HD / 32; ++d) a += q[d] * ((float)k[d * 32 + lane] * ks);
+      a = warp_sum(a) * p.scale_log2 - slope * (float)(at - j);
+      const float mn = fmaxf(m, a), ref = mn == -INFINITY ? 0.f : mn, w0 = exp2f(m - ref), w1 = exp2f(a - ref);
+      m = mn;
+      l = l * w0 + w1;
 #pragma unroll
-    for (int d = 0; d < D; ++d) oa[d] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float ww = exp2f(sm_m[w][g] - ref);
-      la += sm_l[w][g] * ww;
-#pragma unroll
-      for (int d = 0; d < D; ++d) oa[d] += sm_o[w][g][d * 32 + lane] * ww;
-    }
-    if (p.q.k_own) {
-      const float ww = exp2f(own - ref);
-      la += ww;
-#pragma unroll
-      for (int d = 0; d < D; ++d) oa[d] += ww * q_at(p.q, p.q.v_own, (size_t)b * p.q.v_own_stride + (size_t)kvh * HD + d * 32 + lane);
+      for (int d = 0; d < HD / 32; ++d) o[d] = o[d] * w0 + w1 * ((float)v[d * 32 + lane] * vs);
     }
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      const float y = la == 0.f ? 0.f : oa[d] / la;
-      const size_t i = (size_t)b * p.q.out_stride + (size_t)h * HD + d * 32 + lane;
-      if (p.q.dtype == RT_BF16) ((__nv_bfloat16*)p.q.out)[i] = __float2bfloat16_rn(y);
-      else ((float*)p.q.out)[i] = y;
-    }
-    if (p.q.lse && lane == 0) p.q.lse[(size_t)b * p.q.n_heads + h] = la == 0.f ? -INFINITY : (ma + log2f(la)) * 0.6931471805599453f;
+    for (int d = 0; d < HD / 32; ++d) out[g * HD + d * 32 + lane] = o[d];
+    if (lane == 0) { out[kRows * HD + 2 * g] = m; out[kRows * HD + 2 * g + 1] = l; }
   }
+}
+
+// ---- what both kernels end with: the own pair, the division, out and lse ---------------------------
+// A warp finishes query head h of sequence b: m, l and this lane's dimensions d * 32 + lane of o.
+template <int HD>
+__device__ __forceinline__ void finish_head(const PagedAttnParams& p, int b, int h, int lane, float m, float l, float (&o)[HD / 32]) {
+  const int kvh = h / p.group;
+  if (p.q.k_own) {
+    float a = 0.f;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+      a += q_at(p.q.dtype, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + d * 32 + lane) *
+           q_at(p.q.dtype, p.q.k_own, (size_t)b * p.q.k_own_stride + (size_t)kvh * HD + d * 32 + lane);
+    a = warp_sum(a) * p.scale_log2;
+    const float mn = fmaxf(m, a), ref = mn == -INFINITY ? 0.f : mn, w0 = exp2f(m - ref), w1 = exp2f(a - ref);
+    m = mn;
+    l = l * w0 + w1;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+      o[d] = o[d] * w0 + w1 * q_at(p.q.dtype, p.q.v_own, (size_t)b * p.q.v_own_stride + (size_t)kvh * HD + d * 32 + lane);
+  }
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) {
+    const float y = l == 0.f ? 0.f : o[d] / l;
+    const size_t i = (size_t)b * p.q.out_stride + (size_t)h * HD + d * 32 + lane;
+    if (p.q.dtype == RT_BF16) ((__nv_bfloat16*)p.q.out)[i] = __float2bfloat16_rn(y);
+    else ((float*)p.q.out)[i] = y;
+  }
+  if (p.q.lse && lane == 0) p.q.lse[(size_t)b * p.q.n_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// A warp's partial results: slot 0 for the head that it takes over in its middle, slot 1 for the head that it begins and does not end.
+// Of each: rows of o, then (m, l) per row.
+__host__ __device__ inline size_t slot_floats(int rows, int hd) { return (size_t)rows * (hd + 2); }
+
+template <typename CT, int HD, typename Consumer>
+__global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_kernel(const __grid_constant__ PagedAttnParams p, float* part, int part_rows) {
+  using S = Shape<CT, HD>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ long long sums[kWarps * 32], warp_sums[kWarps];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int slices = (p.group + kRows - 1) / kRows, items = p.c.n_kv_heads * slices;
+  const Line ln = scan_line<S::KT, kWarps * 32>(p, items, sums, warp_sums, blockIdx.x == 0);
+  const long long workers = workers_of(ln.total, S::WORKERS);
+  const long long me = (long long)warp * gridDim.x + blockIdx.x;               // neighbours on the line sit on different SMs
+  if (me >= workers) return;
+  const long long u0 = ln.total * me / workers;
+  const int count = (int)(ln.total * (me + 1) / workers - u0);
+
+  // where the line stands at u0
+  Cursor cp;
+  {
+    int lo = 0, hi = kWarps * 32 - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sums[mid] <= u0) lo = mid; else hi = mid - 1;
+    }
+    // (several threads may hold no sequence: the last one whose sum is <= u0 has the unit, or begins behind sequences without units)
+    long long rest = u0 - sums[lo];
+    int b = lo * ln.per;
+    for (;; ++b) {
+      cp.n = clamp_len<S::KT>(p, b);
+      cp.tiles = tiles_of<S::KT>(cp.n);
+      const long long here = (long long)cp.tiles * items;
+      if (rest < here) break;
+      rest -= here;
+    }
+    cp.b = b;
+    cp.item = (int)(rest / cp.tiles);
+    cp.tile = (int)(rest % cp.tiles);
+  }
+  Cursor cc = cp;
+
+  unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
+  const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
+  int pages[S::SUB];
+  auto fetch_pages = [&]() {                                                   // of the producer's unit
+#pragma unroll
+    for (int s = 0; s < S::SUB; ++s) {
+      const int j = cp.tile * S::KT + 16 * s;
+      pages[s] = j < cp.n ? __ldg(p.c.page_table + (size_t)cp.b * p.c.max_pages + (j >> p.log_page)) : -1;
+    }
+  };
+  auto produce = [&](int stage) {
+    const unsigned dst = ring_at + stage * S::STAGE;
+    unsigned char* at = ring + stage * S::STAGE;
+    const int kvh = cp.item / slices;
+#pragma unroll
+    for (int s = 0; s < S::SUB; ++s) {
+      const int j = cp.tile * S::KT + 16 * s;
+      const bool ok = (unsigned)pages[s] < (unsigned)p.c.n_pages;
+      if (!ok && j < cp.n && p.c.status && lane == 0) *p.c.status = RT_ERR_INVALID_ARG;
+      const int live = ok ? min(cp.n - j, 16) : 0;
+      const size_t row = ((size_t)(ok ? pages[s] : 0) * p.c.n_kv_heads + kvh) * p.c.page_size + (ok ? j & (p.c.page_size - 1) : 0);
+      const unsigned char* k = (const unsigned char*)p.c.k + row * S::RB + lane * 16;
+      const unsigned char* v = (const unsigned char*)p.c.v + row * S::RB + lane * 16;
+#pragma unroll
+      for (int i = 0; i < 16 * S::NCH / 32; ++i) {
+        const int id = i * 32 + lane, r = id / S::NCH, ch = id % S::NCH;
+        const int bytes = r < live ? 16 : 0;
+        const size_t off = r < live ? (size_t)i * 512 : 0;
+        copy16(dst + s * 16 * S::RB + key_place<S::NCH>(r, ch) * 16, (r < live ? k : (const unsigned char*)p.c.k) + off, bytes);
+        copy16(dst + (S::KT + s * 16) * S::RB + value_place<S::NCH>(r, ch) * 16, (r < live ? v : (const unsigned char*)p.c.v) + off, bytes);
+      }
+      if (S::EXP && lane < 2) {
+        const uint8_t* e = lane ? p.c.v_exp : p.c.k_exp;
+        copy16(dst + S::KV + lane * S::KT + 16 * s, ok ? e + row : e, ok ? 16 : 0);
+      }
+      if (lane == 0) reinterpret_cast<int*>(at + S::KV + S::EXP)[s] = live;
+    }
+  };
+
+  Consumer con;
+  fetch_pages();
+#pragma unroll
+  for (int s = 0; s < S::STAGES - 1; ++s) {
+    if (s < count) {
+      produce(s);
+      next_unit<S::KT>(p, items, cp);
+      if (s + 1 < count) fetch_pages();
+    }
+    copy_commit();
+  }
+  bool fresh = true;
+  int first_tile = cc.tile;
+  for (int i = 0; i < count; ++i) {
+    copy_wait<S::STAGES - 2>();
+    __syncwarp();
+    if (i + S::STAGES - 1 < count) {
+      produce((i + S::STAGES - 1) % S::STAGES);
+      next_unit<S::KT>(p, items, cp);
+      if (i + S::STAGES < count) fetch_pages();
+    }
+    copy_commit();
+    const int kvh = cc.item / slices, g0 = cc.item % slices * kRows, g_in = min(kRows, p.group - g0), h0 = kvh * p.group + g0;
+    if (fresh) { con.begin(p, cc.b, h0, g_in, lane); first_tile = cc.tile; fresh = false; }
+    unsigned char* st = ring + i % S::STAGES * S::STAGE;
+    int live[S::SUB];
+#pragma unroll
+    for (int s = 0; s < S::SUB; ++s) live[s] = reinterpret_cast<const int*>(st + S::KV + S::EXP)[s];
+    con.unit(p, st, cc.tile * S::KT, p.q.k_own ? cc.n : cc.n - 1, live, lane);
+    const bool ends = cc.tile + 1 == cc.tiles;
+    if (ends || i + 1 == count) {
+      // the stage is used up: it holds the head's results on their way out
+      float* out = reinterpret_cast<float*>(st);
+      __syncwarp();
+      const bool fine = con.dump(out, g_in, lane);
+      __syncwarp();
+      if (!fine) {
+        slow_piece<CT, HD>(p, cc.b, kvh, h0, g_in, first_tile * S::KT, min(cc.n, (cc.tile + 1) * S::KT), p.q.k_own ? cc.n : cc.n - 1, out, lane);
+        __syncwarp();
+      }
+      if (ends && first_tile == 0) {
+        for (int g = 0; g < g_in; ++g) {
+          float x[HD / 32];
+#pragma unroll
+          for (int d = 0; d < HD / 32; ++d) x[d] = out[g * HD + d * 32 + lane];
+          finish_head<HD>(p, cc.b, h0 + g, lane, out[kRows * HD + 2 * g], out[kRows * HD + 2 * g + 1], x);
+        }
+      } else {
+        float* slot = part + ((size_t)me * 2 + (first_tile == 0 ? 1 : 0)) * slot_floats(part_rows, HD);
+        for (int g = 0; g < g_in; ++g) {
+#pragma unroll
+          for (int d = 0; d < HD / 32; ++d) slot[g * HD + d * 32 + lane] = out[g * HD + d * 32 + lane];
+        }
+        if (lane < 2 * g_in) slot[part_rows * HD + lane] = out[kRows * HD + lane];
+      }
+      fresh = true;
+    }
+    next_unit<S::KT>(p, items, cc);
+  }
+}
+
+// Joins the heads that several warps of the kernel above share: a block takes a query head, its warps every kJoinWarps-th partial result.
+constexpr int kJoinWarps = 8;
+template <int KT, int HD>
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __grid_constant__ PagedAttnParams p, const float* part, int part_rows, int max_workers) {
+  __shared__ long long sums[kJoinWarps * 32], warp_sums[kJoinWarps];
+  __shared__ float sm_o[kJoinWarps][HD], sm_m[kJoinWarps], sm_l[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int slices = (p.group + kRows - 1) / kRows, items = p.c.n_kv_heads * slices;
+  const Line ln = scan_line<KT, kJoinWarps * 32>(p, items, sums, warp_sums, false);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (ln.total == 0) return;
+  const long long workers = workers_of(ln.total, max_workers);
+  const long long all = (long long)p.c.n_seqs * p.q.n_heads;
+  for (long long x = blockIdx.x; x < all; x += gridDim.x) {
+    const int b = (int)(x / p.q.n_heads), h = (int)(x % p.q.n_heads);
+    const int n = clamp_len<KT>(p, b);
+    if (n < 0) continue;
+    long long u = sums[b / ln.per];
+    for (int s = b / ln.per * ln.per; s < b; ++s) u += (long long)tiles_of<KT>(clamp_len<KT>(p, s)) * items;
+    const int tiles = tiles_of<KT>(n), g = h % p.group;
+    u += (long long)(h / p.group * slices + g / kRows) * tiles;
+    const long long w0 = worker_of(u, ln.total, workers), w1 = worker_of(u + tiles - 1, ln.total, workers);
+    if (w0 == w1) continue;                                            // written by the warp that held all of it
+    const int r = g % kRows;
+    float m = -INFINITY, l = 0.f, o[HD / 32];
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
+    for (long long w = w0 + warp; w <= w1; w += kJoinWarps) {
+      const float* slot = part + ((size_t)w * 2 + (w == w0 ? 1 : 0)) * slot_floats(part_rows, HD);
+      const float ms = slot[part_rows * HD + 2 * r], ls = slot[part_rows * HD + 2 * r + 1];
+      const float mn = fmaxf(m, ms), ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref), f1 = exp2f(ms - ref);
+      m = mn;
+      l = l * f0 + ls * f1;
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) o[d] = o[d] * f0 + slot[r * HD + d * 32 + lane] * f1;
+    }
+    __syncthreads();                                                   // (the arrays of the head before are read)
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) sm_o[warp][d * 32 + lane] = o[d];
+    if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
+    __syncthreads();
+    if (warp == 0) {
+      float ma = -INFINITY, la = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) ma = fmaxf(ma, sm_m[w]);
+      const float ref = ma == -INFINITY ? 0.f : ma;
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = exp2f(sm_m[w] - ref);
+        la += sm_l[w] * f;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) o[d] += sm_o[w][d * 32 + lane] * f;
+      }
+      finish_head<HD>(p, b, h, lane, ma, la, o);
+    }
+  }
+}
+
+int part_rows_of(int group) { return group < kRows ? group : kRows; }
+
+template <typename CT, int HD, typename Consumer>
+cudaError_t launch_split(const PagedAttnParams& p, float* part, cudaStream_t s) {
+  using S = Shape<CT, HD>;
+  auto* kernel = paged_attn_kernel<CT, HD, Consumer>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  if (e != cudaSuccess) return e;
+  // units there can be at most: no more warps than that
+  const long long slices = ceil_div(p.group, kRows);
+  const long long most = (long long)p.c.n_seqs * p.c.n_kv_heads * slices * max(1LL, ((long long)p.c.max_pages * p.c.page_size + S::KT - 1) / S::KT);
+  const int grid = (int)(most < kSms * S::CTAS ? most : kSms * S::CTAS);
+  kernel<<<grid, kWarps * 32, S::SMEM, s>>>(p, part, part_rows_of(p.group));
+  const cudaError_t e1 = cudaGetLastError();
+  if (e1 != cudaSuccess || most <= (long long)p.c.n_seqs * p.c.n_kv_heads * slices) return e1;
+  const long long heads = (long long)p.c.n_seqs * p.q.n_heads;
+  return launch_chained(paged_join_kernel<S::KT, HD>, dim3((unsigned)(heads < kSms * 4 ? heads : kSms * 4)), dim3(kJoinWarps * 32), 0, s, true, p,
+                        (const float*)part, part_rows_of(p.group), S::WORKERS);
 }
 
 template <typename CT, int HD>
-cudaError_t launch(const PagedAttnParams& p, cudaStream_t s) {
-  const int G = p.group >= 3 ? 4 : p.group;
-  const dim3 grid((unsigned)p.c.n_seqs * (unsigned)p.c.n_kv_heads, ceil_div(p.group, G));
-  if (G == 1) paged_attn_kernel<CT, HD, 1><<<grid, kWarps * 32, 0, s>>>(p);
-  else if (G == 2) paged_attn_kernel<CT, HD, 2><<<grid, kWarps * 32, 0, s>>>(p);
-  else paged_attn_kernel<CT, HD, 4><<<grid, kWarps * 32, 0, s>>>(p);
-  return cudaGetLastError();
+cudaError_t launch_mma(const PagedAttnParams& p, float* part, cudaStream_t s) {
+  return p.q.dtype == RT_F32 ? launch_split<CT, HD, Mma<CT, HD, true>>(p, part, s) : launch_split<CT, HD, Mma<CT, HD, false>>(p, part, s);
+}
+template <int HD>
+cudaError_t launch_simt(const PagedAttnParams& p, float* part, cudaStream_t s) {
+  if (p.group == 1) return launch_split<float, HD, Simt<HD, 1>>(p, part, s);
+  if (p.group == 2) return launch_split<float, HD, Simt<HD, 2>>(p, part, s);
+  if (p.group <= 4) return launch_split<float, HD, Simt<HD, 4>>(p, part, s);
+  return launch_split<float, HD, Simt<HD, 8>>(p, part, s);
 }
 
 }  // namespace
 
-size_t paged_attn_workspace(const rt_paged_cache*, int) { return 256; }
+size_t paged_attn_workspace(const rt_paged_cache* c, int n_heads) {
+  const int hd = c->head_dim, rows = part_rows_of(n_heads / c->n_kv_heads);
+  int workers;
+  if (hd == 64) workers = c->dtype == RT_F32 ? Shape<float, 64>::WORKERS : c->dtype == RT_BF16 ? Shape<__nv_bfloat16, 64>::WORKERS : Shape<__nv_fp8_e4m3, 64>::WORKERS;
+  else workers = c->dtype == RT_F32 ? Shape<float, 128>::WORKERS : c->dtype == RT_BF16 ? Shape<__nv_bfloat16, 128>::WORKERS : Shape<__nv_fp8_e4m3, 128>::WORKERS;
+  return align_up((size_t)workers * 2 * slot_floats(rows, hd) * 4, 256);
+}
 
-cudaError_t paged_attn_launch(const PagedAttnParams& p, void*, cudaStream_t s) {
-  if (p.c.head_dim == 64)
-    return p.c.dtype == RT_F32 ? launch<float, 64>(p, s) : p.c.dtype == RT_BF16 ? launch<__nv_bfloat16, 64>(p, s) : launch<__nv_fp8_e4m3, 64>(p, s);
-  return p.c.dtype == RT_F32 ? launch<float, 128>(p, s) : p.c.dtype == RT_BF16 ? launch<__nv_bfloat16, 128>(p, s) : launch<__nv_fp8_e4m3, 128>(p, s);
+cudaError_t paged_attn_launch(const PagedAttnParams& p, void* workspace, cudaStream_t s) {
+  float* part = (float*)workspace;
+  if (p.c.head_dim == 64) {
+    if (p.c.dtype == RT_F32) return launch_simt<64>(p, part, s);
+    return p.c.dtype == RT_BF16 ? launch_mma<__nv_bfloat16, 64>(p, part, s) : launch_mma<__nv_fp8_e4m3, 64>(p, part, s);
+  }
+  if (p.c.dtype == RT_F32) return launch_simt<128>(p, part, s);
+  return p.c.dtype == RT_BF16 ? launch_mma<__nv_bfloat16, 128>(p, part, s) : launch_mma<__nv_fp8_e4m3, 128>(p, part, s);
 }
 
 }  // namespace rt
