@@ -21,6 +21,8 @@
 //   fp32 pages: CUDA cores, fp32 throughout.
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "rt_paged.h"
 
 namespace rt {
@@ -28,7 +30,7 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 8;      // warps of a block; query heads of a unit
 constexpr int kSms = 148;
-constexpr float kWeightScale = 1024.0f;   // fp16 weights lie in [0, 2^10]: their second term keeps 2^-35 of the largest
+constexpr float kWeightLog2 = 10.0f;      // fp16 weights lie in [0, 2^10]: their second term keeps 2^-35 of the largest
 
 // ---- shapes ------------------------------------------------------------------------------------
 template <typename CT, int HD>
@@ -38,8 +40,8 @@ struct Shape {
   static constexpr int SUB = KT / 16;
   static constexpr int KV = 2 * KT * RB;
   static constexpr int EXP = sizeof(CT) == 1 ? 2 * KT : 0;
-  static constexpr int STAGE = (KV + EXP + 16 + 127) / 128 * 128 < kRows * (HD + 2) * 4 ? (kRows * (HD + 2) * 4 + 127) / 128 * 128
-                                                                                         : (KV + EXP + 16 + 127) / 128 * 128;
+  static constexpr int OUT = kRows * (HD + 2) * 4;                           // a used stage also carries a head's results
+  static constexpr int STAGE = ((KV + EXP > OUT ? KV + EXP : OUT) + 127) / 128 * 128;
   static constexpr int STAGES = KV <= 4096 ? 4 : 3;
   static constexpr int CTAS = KV <= 4096 ? 3 : KV <= 8192 ? 2 : 1;           // blocks of an SM (shared memory)
   static constexpr int SMEM = kWarps * STAGES * STAGE;
@@ -100,6 +102,7 @@ __device__ __forceinline__ long long workers_of(long long total, int workers) { 
 __device__ __forceinline__ long long worker_of(long long u, long long total, long long w) { return ((u + 1) * w - 1) / total; }
 
 struct Cursor { int b, item, tile, tiles, n; };      // item = head of the cache * slices + slice of its query heads
+__device__ __forceinline__ int head_of(int item, int slices) { return slices == 1 ? item : item / slices; }
 
 template <int KT>
 __device__ __forceinline__ void next_unit(const PagedAttnParams& p, int items, Cursor& c) {
@@ -115,6 +118,11 @@ __device__ __forceinline__ void next_unit(const PagedAttnParams& p, int items, C
 }
 
 // ---- small pieces ------------------------------------------------------------------------------
+__device__ __forceinline__ float ex2(float x) {        // 2^x to 2^-22, 0 below 2^-126
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float q_at(int dtype, const void* p, size_t i) {
   return dtype == RT_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : ((const float*)p)[i];
 }
@@ -234,9 +242,11 @@ struct Mma {
       for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
   }
 
-  // one staged unit: positions j0 .. j0 + KT, of which live[s] of the s-th sixteen count; the query is at position `at`
-  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, const int (&live)[S::SUB], int lane) {
+  // One staged unit: positions j0 .. j0 + KT; the first `live` count, but not the sixteens whose bit is
+  // set in `bad`; the query is at position `at`.
+  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, int live, unsigned bad, int lane) {
     const int r = lane >> 2, c = lane & 3;
+    const bool slopes = p.q.alibi_slopes != nullptr;
     float s[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -264,33 +274,42 @@ struct Mma {
         }
       }
     }
-    // scores in log2 units, the maximum of the row, weights
-    const uint8_t* ke = st + S::KV;
-    const uint8_t* ve = ke + S::KT;
-    float a[NT][2], vs[NT][2], top = m, topv = mv;
+    // scores in log2 units (for F8 also those of the scaled weights), the maximum of the row, weights
+    float a[NT][2], av[F8 ? NT : 1][2], top = m, topv = mv;
+    const float far = slopes ? (float)(j0 + 2 * c - at) : 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       unsigned kx = 0, vx = 0;
       if (F8) {
-        kx = *reinterpret_cast<const uint16_t*>(ke + 8 * t + 2 * c);
-        vx = *reinterpret_cast<const uint16_t*>(ve + 8 * t + 2 * c);
+        kx = *reinterpret_cast<const uint16_t*>(st + S::KV + 8 * t + 2 * c);
+        vx = *reinterpret_cast<const uint16_t*>(st + S::KV + S::KT + 8 * t + 2 * c);
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float x = TERMS > 1 ? s[t][e] + s[t][e + 2] : s[t][e];
-        x *= q_scale;
-        const int j = 8 * t + 2 * c + e;
-        const unsigned kb = (kx >> (8 * e)) & 0xffu, vb = (vx >> (8 * e)) & 0xffu;
-        if (F8) x *= scale_of(kb);
-        x -= slope * (float)(at - j0 - j);
-        a[t][e] = (j & 15) < live[t / 2] ? x : -INFINITY;
-        top = fmaxf(top, a[t][e]);
-        if (F8) {
-          vs[t][e] = scale_of(vb);
-          topv = fmaxf(topv, a[t][e] + (float)((int)vb - 127));
-        }
+        x *= F8 ? q_scale * __uint_as_float((e ? kx << 15 : kx << 23) & 0x7f800000u) : q_scale;
+        if (slopes) x = fmaf(slope, far + (float)(8 * t + e), x);
+        a[t][e] = x;
+        if (F8) av[F8 ? t : 0][e] = x + (__uint_as_float(__byte_perm(vx, 0x4b000000u, e ? 0x7551u : 0x7550u)) - 8388735.f);     // 2^23 + exponent - (2^23 + 127)
       }
     }
+    if (live < S::KT || bad) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (8 * t + 2 * c + e >= live || (bad >> (t / 2) & 1)) {
+            a[t][e] = -INFINITY;
+            if (F8) av[F8 ? t : 0][e] = -INFINITY;
+          }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top = fmaxf(top, a[t][e]);
+        if (F8) topv = fmaxf(topv, av[F8 ? t : 0][e]);
+      }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     if (F8) {
@@ -298,8 +317,8 @@ struct Mma {
       topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, 2));
     }
     if (__any_sync(0xffffffffu, top > m || (F8 && topv > mv))) {
-      const float w = m == -INFINITY ? 0.f : exp2f(m - top);
-      const float wo = F8 ? (mv == -INFINITY ? 0.f : exp2f(mv - topv)) : w;
+      const float w = m == -INFINITY ? 0.f : ex2(m - top);
+      const float wo = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - topv)) : w;
       l *= w;
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j)
@@ -308,17 +327,16 @@ struct Mma {
       m = top;
       mv = topv;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
-    const float to16 = !F8 ? 1.f : mv == -INFINITY ? 0.f : kWeightScale * exp2f(m - mv);
+    const float ref = m == -INFINITY ? 0.f : m, refv = mv == -INFINITY ? 0.f : mv - kWeightLog2;
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
       float w[4];                          // positions 2c, 2c + 1, 8 + 2c, 9 + 2c of the sixteen
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int t = 2 * sub + e / 2;
-        w[e] = exp2f(a[t][e & 1] - ref);
+        w[e] = ex2(a[t][e & 1] - ref);
         l += w[e];
-        if (F8) w[e] = w[e] * vs[t][e & 1] * to16;
+        if (F8) w[e] = ex2(av[F8 ? t : 0][e & 1] - refv);
       }
       unsigned w0[2], w1[2], w2[2];
 #pragma unroll
@@ -388,7 +406,7 @@ struct Mma {
     float all = 0.f;
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
-    const float back = F8 ? (mv == -INFINITY ? 0.f : exp2f(mv - m) * (1.f / kWeightScale)) : 1.f;
+    const float back = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - m - kWeightLog2)) : 1.f;
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
 #pragma unroll
@@ -427,12 +445,12 @@ struct Simt {
       }
     }
   }
-  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, const int (&live)[S::SUB], int lane) {
+  __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, int live, unsigned bad, int lane) {
     const int sub = lane / LPK, c = lane % LPK;
 #pragma unroll 4
     for (int i = 0; i < 16 / KPI; ++i) {
       const int j = i * KPI + sub;
-      const bool ok = j < live[0];
+      const bool ok = j < live && !bad;
       const float4 k = reinterpret_cast<const float4*>(st)[key_place<S::NCH>(j, c)];
       const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH>(j, c)];
 #pragma unroll
@@ -442,7 +460,7 @@ struct Simt {
         for (int w = LPK / 2; w; w >>= 1) a += __shfl_xor_sync(0xffffffffu, a, w);
         a = ok ? a * p.scale_log2 - slope[g] * (float)(at - j0 - j) : -INFINITY;
         const float mn = fmaxf(m[g], a), ref = mn == -INFINITY ? 0.f : mn;
-        const float w0 = exp2f(m[g] - ref), w1 = exp2f(a - ref);
+        const float w0 = ex2(m[g] - ref), w1 = ex2(a - ref);
         m[g] = mn;
         l[g] = l[g] * w0 + w1;
         o[g][0] = o[g][0] * w0 + w1 * v.x; o[g][1] = o[g][1] * w0 + w1 * v.y;      // (rows that do not count are zeros)
@@ -579,7 +597,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
 
   unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
   const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
-  int pages[S::SUB];
+  int pages[S::SUB], kvh = head_of(cp.item, slices);
+  unsigned bad = 0;                                                            // SUB bits a stage: pages that do not exist
   auto fetch_pages = [&]() {                                                   // of the producer's unit
 #pragma unroll
     for (int s = 0; s < S::SUB; ++s) {
@@ -589,31 +608,46 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
   };
   auto produce = [&](int stage) {
     const unsigned dst = ring_at + stage * S::STAGE;
-    unsigned char* at = ring + stage * S::STAGE;
-    const int kvh = cp.item / slices;
+    bad &= ~(((1u << S::SUB) - 1) << (stage * S::SUB));
 #pragma unroll
     for (int s = 0; s < S::SUB; ++s) {
       const int j = cp.tile * S::KT + 16 * s;
       const bool ok = (unsigned)pages[s] < (unsigned)p.c.n_pages;
-      if (!ok && j < cp.n && p.c.status && lane == 0) *p.c.status = RT_ERR_INVALID_ARG;
-      const int live = ok ? min(cp.n - j, 16) : 0;
-      const size_t row = ((size_t)(ok ? pages[s] : 0) * p.c.n_kv_heads + kvh) * p.c.page_size + (ok ? j & (p.c.page_size - 1) : 0);
+      const size_t row = ((size_t)(ok ? pages[s] : 0) * p.c.n_kv_heads + kvh) * p.c.page_size + (j & (p.c.page_size - 1));
       const unsigned char* k = (const unsigned char*)p.c.k + row * S::RB + lane * 16;
       const unsigned char* v = (const unsigned char*)p.c.v + row * S::RB + lane * 16;
+      const unsigned kd = dst + s * 16 * S::RB, vd = kd + S::KT * S::RB;
+      if (ok && j + 16 <= cp.n) {
 #pragma unroll
-      for (int i = 0; i < 16 * S::NCH / 32; ++i) {
-        const int id = i * 32 + lane, r = id / S::NCH, ch = id % S::NCH;
-        const int bytes = r < live ? 16 : 0;
-        const size_t off = r < live ? (size_t)i * 512 : 0;
-        copy16(dst + s * 16 * S::RB + key_place<S::NCH>(r, ch) * 16, (r < live ? k : (const unsigned char*)p.c.k) + off, bytes);
-        copy16(dst + (S::KT + s * 16) * S::RB + value_place<S::NCH>(r, ch) * 16, (r < live ? v : (const unsigned char*)p.c.v) + off, bytes);
+        for (int i = 0; i < S::NCH / 2; ++i) {
+          const int row_in = 32 / S::NCH * i + lane / S::NCH, ch = lane % S::NCH;
+          copy16(kd + key_place<S::NCH>(row_in, ch) * 16, k + i * 512, 16);
+          copy16(vd + value_place<S::NCH>(row_in, ch) * 16, v + i * 512, 16);
+        }
+      } else {
+        const int live = ok ? cp.n - j : 0;
+        if (!ok) {
+          bad |= 1u << (stage * S::SUB + s);
+          if (j < cp.n && p.c.status && lane == 0) *p.c.status = RT_ERR_INVALID_ARG;
+        }
+#pragma unroll 1
+        for (int i = 0; i < S::NCH / 2; ++i) {
+          const int row_in = (i * 32 + lane) / S::NCH, ch = lane % S::NCH;
+          const bool in = row_in < live;
+          copy16(kd + key_place<S::NCH>(row_in, ch) * 16, in ? k + i * 512 : (const unsigned char*)p.c.k, in ? 16 : 0);
+          copy16(vd + value_place<S::NCH>(row_in, ch) * 16, in ? v + i * 512 : (const unsigned char*)p.c.v, in ? 16 : 0);
+        }
       }
       if (S::EXP && lane < 2) {
         const uint8_t* e = lane ? p.c.v_exp : p.c.k_exp;
         copy16(dst + S::KV + lane * S::KT + 16 * s, ok ? e + row : e, ok ? 16 : 0);
       }
-      if (lane == 0) reinterpret_cast<int*>(at + S::KV + S::EXP)[s] = live;
     }
+  };
+  auto advance = [&]() {
+    const int before = cp.item;
+    next_unit<S::KT>(p, items, cp);
+    if (cp.item != before) kvh = head_of(cp.item, slices);
   };
 
   Consumer con;
@@ -622,38 +656,41 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
   for (int s = 0; s < S::STAGES - 1; ++s) {
     if (s < count) {
       produce(s);
-      next_unit<S::KT>(p, items, cp);
+      advance();
       if (s + 1 < count) fetch_pages();
     }
     copy_commit();
   }
   bool fresh = true;
-  int first_tile = cc.tile;
-  for (int i = 0; i < count; ++i) {
+  int first_tile = cc.tile, stage = 0;
+  for (int i = 0; i < count; ++i, stage = stage + 1 == S::STAGES ? 0 : stage + 1) {
     copy_wait<S::STAGES - 2>();
     __syncwarp();
     if (i + S::STAGES - 1 < count) {
-      produce((i + S::STAGES - 1) % S::STAGES);
-      next_unit<S::KT>(p, items, cp);
+      produce(stage == 0 ? S::STAGES - 1 : stage - 1);
+      advance();
       if (i + S::STAGES < count) fetch_pages();
     }
     copy_commit();
-    const int kvh = cc.item / slices, g0 = cc.item % slices * kRows, g_in = min(kRows, p.group - g0), h0 = kvh * p.group + g0;
-    if (fresh) { con.begin(p, cc.b, h0, g_in, lane); first_tile = cc.tile; fresh = false; }
-    unsigned char* st = ring + i % S::STAGES * S::STAGE;
-    int live[S::SUB];
-#pragma unroll
-    for (int s = 0; s < S::SUB; ++s) live[s] = reinterpret_cast<const int*>(st + S::KV + S::EXP)[s];
-    con.unit(p, st, cc.tile * S::KT, p.q.k_own ? cc.n : cc.n - 1, live, lane);
+    if (fresh) {
+      const int g0 = (slices == 1 ? 0 : cc.item % slices) * kRows;
+      con.begin(p, cc.b, head_of(cc.item, slices) * p.group + g0, min(kRows, p.group - g0), lane);
+      first_tile = cc.tile;
+      fresh = false;
+    }
+    unsigned char* st = ring + stage * S::STAGE;
+    con.unit(p, st, cc.tile * S::KT, p.q.k_own ? cc.n : cc.n - 1, cc.n - cc.tile * S::KT, bad >> (stage * S::SUB) & ((1u << S::SUB) - 1), lane);
     const bool ends = cc.tile + 1 == cc.tiles;
     if (ends || i + 1 == count) {
       // the stage is used up: it holds the head's results on their way out
+      const int kv_head = head_of(cc.item, slices), g0 = (slices == 1 ? 0 : cc.item % slices) * kRows, g_in = min(kRows, p.group - g0),
+                h0 = kv_head * p.group + g0;
       float* out = reinterpret_cast<float*>(st);
       __syncwarp();
       const bool fine = con.dump(out, g_in, lane);
       __syncwarp();
       if (!fine) {
-        slow_piece<CT, HD>(p, cc.b, kvh, h0, g_in, first_tile * S::KT, min(cc.n, (cc.tile + 1) * S::KT), p.q.k_own ? cc.n : cc.n - 1, out, lane);
+        slow_piece<CT, HD>(p, cc.b, kv_head, h0, g_in, first_tile * S::KT, min(cc.n, (cc.tile + 1) * S::KT), p.q.k_own ? cc.n : cc.n - 1, out, lane);
         __syncwarp();
       }
       if (ends && first_tile == 0) {
@@ -743,8 +780,14 @@ template <typename CT, int HD, typename Consumer>
 cudaError_t launch_split(const PagedAttnParams& p, float* part, cudaStream_t s) {
   using S = Shape<CT, HD>;
   auto* kernel = paged_attn_kernel<CT, HD, Consumer>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-  if (e != cudaSuccess) return e;
+  static std::atomic<unsigned long long> set{0};         // devices on which the kernel has its shared memory
+  int dev = 0;
+  if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+  if (dev > 63 || !(set.load(std::memory_order_relaxed) >> dev & 1)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != cudaSuccess) return e;
+    if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
   // units there can be at most: no more warps than that
   const long long slices = ceil_div(p.group, kRows);
   const long long most = (long long)p.c.n_seqs * p.c.n_kv_heads * slices * max(1LL, ((long long)p.c.max_pages * p.c.page_size + S::KT - 1) / S::KT);

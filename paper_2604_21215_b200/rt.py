@@ -321,15 +321,20 @@ def _require(ok: bool, where: str):
         raise RtError(RT_ERR_INVALID_ARG, where)
 
 
+def _raw_stream(index: int) -> int:
+    """The current stream of a device as a cudaStream_t (torch.cuda.current_stream builds an object for it, 2 us)."""
+    return _torch()._C._cuda_getCurrentRawStream(index)
+
+
 def _rows(t, heads: int, head_dim: int, n: int, dtype, device, where: str) -> tuple:
     """(address, stride) of [n, heads, head_dim] or [n, heads * head_dim] rows whose heads are contiguous."""
-    _require(t.dtype == dtype and t.device == device and t.shape[0] == n and t.numel() == n * heads * head_dim, where)
     st, sh = t.stride(), t.shape
     if len(sh) == 3:
-        ok = sh[1] == heads and (st[2] == 1 or head_dim == 1) and (heads == 1 or st[1] == head_dim)
+        ok = sh[1] == heads and sh[2] == head_dim and st[2] == 1 and (heads == 1 or st[1] == head_dim)
     else:
-        ok = len(sh) == 2 and st[1] == 1
-    _require(ok or n == 0, where)
+        ok = len(sh) == 2 and sh[1] == heads * head_dim and st[1] == 1
+    if not ok or sh[0] != n or t.dtype != dtype or t.device != device:
+        raise RtError(RT_ERR_INVALID_ARG, where)
     return t.data_ptr(), st[0]
 
 
@@ -337,7 +342,8 @@ def _vector(t, n: int, dtype, device, where: str):
     """Address of a contiguous array of n elements, None for None."""
     if t is None:
         return None
-    _require(t.dtype == dtype and t.device == device and t.numel() == n and t.is_contiguous(), where)
+    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise RtError(RT_ERR_INVALID_ARG, where)
     return t.data_ptr()
 
 
@@ -603,6 +609,7 @@ class PagedCache:
         self._c = RtPagedCache(k.data_ptr(), v.data_ptr(), _vector(k_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": k_exp"),
                                _vector(v_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": v_exp"), page_table.data_ptr(),
                                self._status.data_ptr(), n_pages, page, n_kv, hd, code, page_table.shape[0], page_table.shape[1])
+        self._index = k.device.index
         self._codes = {torch.float32: RT_F32, torch.bfloat16: RT_BF16}
         self._need: dict = {}                          # workspace bytes by number of query heads
         _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, where + ": shape")
@@ -618,25 +625,27 @@ class PagedCache:
         exps = lambda: torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == "e4m3" else None
         return cls(pool(), pool(), torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), exps(), exps())
 
-    def _stream(self) -> int:
-        return _torch().cuda.current_stream(self.device).cuda_stream
-
     def write(self, k, v, seq, pos) -> None:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
         seq[r] (int32); a negative position skips the row."""
         torch, c, n = _torch(), self._c, k.shape[0]
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.write(k, v, seq, pos)
         where = "PagedCache.write"
         _require(k.dtype in self._codes, where + ": k")
         kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": k")
         vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": v")
         sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
-        with torch.cuda.device(self.device):
-            _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, self._stream()), "rt_cache_write")
+        _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, _raw_stream(self._index)), "rt_cache_write")
 
     def read(self, seq, pos, dtype: str = "bf16", k=None, v=None):
         """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
         Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
         torch, c, n = _torch(), self._c, pos.shape[0]
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.read(seq, pos, dtype, k, v)
         where, t = "PagedCache.read", _tdtype(dtype)
         shape = (n, c.n_kv_heads, c.head_dim)
         k = torch.empty(shape, dtype=t, device=self.device) if k is None else k
@@ -644,8 +653,7 @@ class PagedCache:
         kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": k")
         vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": v")
         sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
-        with torch.cuda.device(self.device):
-            _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, self._stream()), "rt_cache_read")
+        _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, _raw_stream(self._index)), "rt_cache_read")
         return k, v
 
     def attend(self, q, lens, k_own=None, v_own=None, scale: Optional[float] = None, alibi_slopes=None, out=None, lse=None):
@@ -654,10 +662,13 @@ class PagedCache:
         [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
         whatever the memory holds)."""
         torch, c = _torch(), self._c
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.attend(q, lens, k_own, v_own, scale, alibi_slopes, out, lse)
         where, B, hd = "PagedCache.attend", c.n_seqs, c.head_dim
         _require(q.dtype in self._codes and q.dim() == 3, where + ": q")
         H, t = q.shape[1], q.dtype
-        out = torch.empty((B, H, hd), dtype=t, device=self.device) if out is None else out
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         a = RtPagedQuery()
         a.q, a.q_stride = _rows(q, H, hd, B, t, self.device, where + ": q")
         a.out, a.out_stride = _rows(out, H, hd, B, t, self.device, where + ": out")
@@ -674,8 +685,7 @@ class PagedCache:
             need = self._need[H] = rt_paged_attention_workspace_bytes(c, H)
             _require(need > 0, where + ": q")
         ws = torch.empty(need, dtype=torch.uint8, device=self.device)       # of its own for every call: calls on two streams may overlap
-        with torch.cuda.device(self.device):
-            _check(rt_paged_attention(c, a, ws.data_ptr(), need, self._stream()), "rt_paged_attention")
+        _check(rt_paged_attention(c, a, ws.data_ptr(), need, _raw_stream(self._index)), "rt_paged_attention")
         return out
 
     def status(self) -> int:
@@ -691,7 +701,7 @@ class QkRotate:
     def __init__(self, n_heads: int, n_kv_heads: int, dtype: str = "bf16", head_dim: int = 64, rot_dim: Optional[int] = None,
                  base: float = 10000.0, freq: Optional[Sequence[float]] = None, pairs: str = "halves", norm: bool = True,
                  rms_eps: float = 1e-6):
-        self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = dtype, n_heads, n_kv_heads, head_dim
+        self.dtype, self.n_heads, self.n_kv_heads, self.head_dim, self._t = dtype, n_heads, n_kv_heads, head_dim, _tdtype(dtype)
         rot_dim = head_dim if rot_dim is None else rot_dim
         freq = [base ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)] if freq is None else list(freq)
         _require(len(freq) == rot_dim // 2, "QkRotate: freq")
@@ -701,7 +711,7 @@ class QkRotate:
         _require(rt_qk_rotate_backward_workspace_bytes(self.cfg, 1) > 0, "QkRotate: shape")
 
     def _inputs(self, q, k, pos, g_q, g_k, where):
-        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], _tdtype(self.dtype), q.device
+        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], self._t, q.device
         _require(q.is_cuda and (k is not None or self.n_kv_heads == 0), where + ": q, k")
         qp, qs = _rows(q, self.n_heads, hd, n, t, dev, where + ": q")
         kp, ks = _rows(k, self.n_kv_heads, hd, n, t, dev, where + ": k") if self.n_kv_heads else (None, 0)
@@ -712,36 +722,38 @@ class QkRotate:
         """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
         and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
         torch = _torch()
+        if q.is_cuda and torch.cuda.current_device() != q.device.index:
+            with torch.cuda.device(q.device):
+                return self.forward(q, k, pos, g_q, g_k, q_out, k_out)
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, "QkRotate.forward")
-        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=t, device=dev) if q_out is None else q_out
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
         qo, qos = _rows(q_out, self.n_heads, self.head_dim, n, t, dev, "QkRotate.forward: q_out")
         ko, kos = None, 0
         if self.n_kv_heads:
-            k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=t, device=dev) if k_out is None else k_out
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
             ko, kos = _rows(k_out, self.n_kv_heads, self.head_dim, n, t, dev, "QkRotate.forward: k_out")
-        with torch.cuda.device(dev):
-            _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, torch.cuda.current_stream(dev).cuda_stream),
-                   "rt_qk_rotate")
+        _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, _raw_stream(dev.index)), "rt_qk_rotate")
         return q_out, k_out
 
     def backward(self, q, k, pos, dq_out, dk_out, g_q=None, g_k=None, dq=None, dk=None):
         """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
         gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
         torch = _torch()
-        where, f32, hd = "QkRotate.backward", _torch().float32, self.head_dim
+        if q.is_cuda and torch.cuda.current_device() != q.device.index:
+            with torch.cuda.device(q.device):
+                return self.backward(q, k, pos, dq_out, dk_out, g_q, g_k, dq, dk)
+        where, f32, hd = "QkRotate.backward", torch.float32, self.head_dim
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, where)
         kn = n * self.n_kv_heads * hd
-        new = lambda heads: torch.empty((n, heads, hd), dtype=f32, device=dev)
-        dq = new(self.n_heads) if dq is None else dq
-        dk = (new(self.n_kv_heads) if dk is None else dk) if self.n_kv_heads else None
-        dgq = None if g_q is None else torch.empty(self.n_heads * hd, dtype=f32, device=dev)
-        dgk = None if g_k is None or not self.n_kv_heads else torch.empty(self.n_kv_heads * hd, dtype=f32, device=dev)
+        dq = torch.empty_like(dq_out) if dq is None else dq
+        dk = (torch.empty_like(dk_out) if dk is None else dk) if self.n_kv_heads else None
+        dgq = None if g_q is None else torch.empty_like(g_q, dtype=f32)
+        dgk = None if g_k is None or not self.n_kv_heads else torch.empty_like(g_k, dtype=f32)
         ptr = lambda x: None if x is None else x.data_ptr()
         ws = torch.empty(rt_qk_rotate_backward_workspace_bytes(self.cfg, n), dtype=torch.uint8, device=dev)
-        with torch.cuda.device(dev):
-            _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, where + ": dq_out"),
-                                         _vector(dk_out, kn, f32, dev, where + ": dk_out") if kn else None,
-                                         _vector(dq, n * self.n_heads * hd, f32, dev, where + ": dq"),
-                                         _vector(dk, kn, f32, dev, where + ": dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
-                                         torch.cuda.current_stream(dev).cuda_stream), "rt_qk_rotate_backward")
+        _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, where + ": dq_out"),
+                                     _vector(dk_out, kn, f32, dev, where + ": dk_out") if kn else None,
+                                     _vector(dq, n * self.n_heads * hd, f32, dev, where + ": dq"),
+                                     _vector(dk, kn, f32, dev, where + ": dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
+                                     _raw_stream(dev.index)), "rt_qk_rotate_backward")
         return dq, dk, dgq, dgk

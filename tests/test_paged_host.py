@@ -91,6 +91,8 @@ def test_rows_to_rotate_that_are_refused():
     assert call(rows=0) == rt.RT_OK
     need = rt.rt_qk_rotate_backward_workspace_bytes(config(), 1000)
     assert need >= rt.rt_qk_rotate_backward_workspace_bytes(config(), 10) >= rt.rt_qk_rotate_backward_workspace_bytes(config(), 0) > 0
+    sizes = [rt.rt_qk_rotate_backward_workspace_bytes(config(), r) for r in (0, 1, 16, 17, 1000, 18943, 18944, 18945, 40000, 1 << 30)]
+    assert sizes == sorted(sizes)                              # a workspace for many rows serves fewer
     grad = dict(q=ADDR, k=ADDR, qs=256, ks=128, gq=None, gk=None, pos=ADDR, rows=1000, dqo=ADDR, dko=ADDR, dq=ADDR, dk=ADDR, dgq=None, dgk=None, ws=ADDR, n=need)
     call = lambda **kw: rt.rt_qk_rotate_backward(config(), *{**grad, **kw}.values(), None)
     for kw in (dict(q=None), dict(dqo=None), dict(dko=None), dict(dq=None), dict(dk=None), dict(dqo=ADDR + 4), dict(dk=ADDR + 8), dict(dgq=ADDR + 4), dict(ws=None),
