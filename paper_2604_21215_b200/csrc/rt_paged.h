@@ -26,6 +26,7 @@ struct PagedAttnParams {
   float scale_log2;
 };
 cudaError_t paged_attn_launch(const PagedAttnParams& p, void* workspace, cudaStream_t s);
+bool paged_attn_counts(const rt_paged_cache* c, int n_heads);      // whether 32 bits count what such a call can be asked to do
 size_t paged_attn_workspace(const rt_paged_cache* c, int n_heads);
 
 constexpr int kMaxRot = 128;

@@ -24,7 +24,8 @@ rt_status cache_ok(const rt_paged_cache* c) {
   if (!aligned4(c->page_table) || !aligned4(c->status)) return RT_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return RT_ERR_UNSUPPORTED;
   if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return RT_ERR_UNSUPPORTED;
-  if (c->n_kv_heads > 65535 || (long long)c->n_seqs * c->n_kv_heads > INT32_MAX) return RT_ERR_UNSUPPORTED;
+  // (a page's bytes and the heads of all sequences are counted in 32 bits)
+  if ((long long)c->n_kv_heads * c->page_size * c->head_dim > INT32_MAX / 4 || (long long)c->n_seqs * c->n_kv_heads > INT32_MAX) return RT_ERR_UNSUPPORTED;
   return RT_OK;
 }
 
@@ -105,7 +106,7 @@ rt_status rt_cache_read(const rt_paged_cache* cache, int32_t dtype, void* k, voi
 }
 
 size_t rt_paged_attention_workspace_bytes(const rt_paged_cache* cache, int32_t n_heads) {
-  if (cache_ok(cache) != RT_OK || n_heads <= 0 || n_heads % cache->n_kv_heads) return 0;
+  if (cache_ok(cache) != RT_OK || n_heads <= 0 || n_heads % cache->n_kv_heads || !paged_attn_counts(cache, n_heads)) return 0;
   return paged_attn_workspace(cache, n_heads);
 }
 
@@ -120,7 +121,7 @@ rt_status rt_paged_attention(const rt_paged_cache* cache, const rt_paged_query* 
   if ((q->k_own != nullptr) != (q->v_own != nullptr)) return RT_ERR_INVALID_ARG;
   if (q->k_own && (!rows_ok(q->k_own, q->dtype, q->k_own_stride, kv_row, B) || !rows_ok(q->v_own, q->dtype, q->v_own_stride, kv_row, B)))
     return RT_ERR_INVALID_ARG;
-  if (q->n_heads / cache->n_kv_heads > 1024) return RT_ERR_UNSUPPORTED;
+  if (q->n_heads / cache->n_kv_heads > 1024 || !paged_attn_counts(cache, q->n_heads)) return RT_ERR_UNSUPPORTED;
   if (workspace_bytes < paged_attn_workspace(cache, q->n_heads)) return RT_ERR_WORKSPACE;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   PagedAttnParams p;

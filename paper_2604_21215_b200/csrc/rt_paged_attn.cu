@@ -42,19 +42,28 @@ struct Shape {
   static constexpr int EXP = sizeof(CT) == 1 ? 2 * KT : 0;
   static constexpr int OUT = kRows * (HD + 2) * 4;                           // a used stage also carries a head's results
   static constexpr int STAGE = ((KV + EXP > OUT ? KV + EXP : OUT) + 127) / 128 * 128;
-  static constexpr int STAGES = KV <= 4096 ? 4 : 3;
-  static constexpr int CTAS = KV <= 4096 ? 3 : KV <= 8192 ? 2 : 1;           // blocks of an SM (shared memory)
+  // Units of a ring, and blocks of an SM (both limited by the SM's 227 KB, and by 65,536 registers).  Twelve warps an SM hide a unit's chain of products,
+  // maxima and exponentials better than eight with a deeper ring; heads of 128 in bf16 need the registers of eight.
+  static constexpr bool SMALL = HD == 64 && sizeof(CT) == 2;
+  static constexpr int STAGES = KV <= 4096 ? 4 : SMALL ? 2 : 3;
+  static constexpr int CTAS = KV <= 4096 || SMALL ? 3 : KV <= 8192 ? 2 : 1;
   static constexpr int SMEM = kWarps * STAGES * STAGE;
   static constexpr int WORKERS = kSms * CTAS * kWarps;
 };
 
 // ---- the line of units -------------------------------------------------------------------------
+// (units are counted in 32 bits: paged_attn_launch refuses caches that could hold more)
 struct Line {
-  int per;              // sequences per thread of the scan
-  long long total;
+  int per;                      // sequences per thread of the scan
+  unsigned total, workers;      // units, and the warps that share them: `more` of them take each + 1 units, the others `each`
+  unsigned each, more;
+  __device__ __forceinline__ unsigned begin(unsigned w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ unsigned worker_of(unsigned u) const {
+    const unsigned long_part = more * (each + 1);
+    return u < long_part ? u / (each + 1) : more + (u - long_part) / each;
+  }
 };
 
-template <int KT>
 __device__ __forceinline__ int clamp_len(const PagedAttnParams& p, int b) {
   const int n = __ldg(p.q.lens + b);
   const long long room = (long long)p.c.max_pages << p.log_page;
@@ -63,29 +72,29 @@ __device__ __forceinline__ int clamp_len(const PagedAttnParams& p, int b) {
 template <int KT>
 __device__ __forceinline__ int tiles_of(int n) { return n < 0 ? 0 : max(1, (n + KT - 1) / KT); }
 
-// Units before each thread's first sequence, in sum[] (THREADS entries), and the total.  All threads of the block call.
+// Units before each thread's first sequence, in sum[] (THREADS entries), and the line.  All threads of the block call.
 template <int KT, int THREADS>
-__device__ __forceinline__ Line scan_line(const PagedAttnParams& p, int items, long long* sum, long long* warp_sums, bool report) {
+__device__ __forceinline__ Line scan_line(const PagedAttnParams& p, int items, int max_workers, unsigned* sum, unsigned* warp_sums, bool report) {
   Line ln;
   ln.per = (p.c.n_seqs + THREADS - 1) / THREADS;
   const int b0 = threadIdx.x * ln.per;
-  long long mine = 0;
+  unsigned mine = 0;
   const long long room = (long long)p.c.max_pages << p.log_page;
   for (int b = b0; b < min(b0 + ln.per, p.c.n_seqs); ++b) {
     const int n = __ldg(p.q.lens + b);
     if (report && n > room && p.c.status) *p.c.status = RT_ERR_INVALID_ARG;
-    mine += (long long)tiles_of<KT>(clamp_len<KT>(p, b)) * items;
+    mine += (unsigned)tiles_of<KT>(n > room ? (int)room : n) * items;
   }
-  long long inc = mine;
+  unsigned inc = mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long t = __shfl_up_sync(0xffffffffu, inc, o);
+    const unsigned t = __shfl_up_sync(0xffffffffu, inc, o);
     if (lane >= o) inc += t;
   }
   if (lane == 31) warp_sums[warp] = inc;
   __syncthreads();
-  long long before = 0, total = 0;
+  unsigned before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
     if (w < warp) before += warp_sums[w];
@@ -94,12 +103,11 @@ __device__ __forceinline__ Line scan_line(const PagedAttnParams& p, int items, l
   sum[threadIdx.x] = before + inc - mine;
   __syncthreads();
   ln.total = total;
+  ln.workers = min(total, (unsigned)max_workers);
+  ln.each = ln.workers ? total / ln.workers : 0;
+  ln.more = total - ln.each * ln.workers;
   return ln;
 }
-
-// how many warps share the line, and which one holds a unit
-__device__ __forceinline__ long long workers_of(long long total, int workers) { return total < workers ? total : workers; }
-__device__ __forceinline__ long long worker_of(long long u, long long total, long long w) { return ((u + 1) * w - 1) / total; }
 
 struct Cursor { int b, item, tile, tiles, n; };      // item = head of the cache * slices + slice of its query heads
 __device__ __forceinline__ int head_of(int item, int slices) { return slices == 1 ? item : item / slices; }
@@ -112,7 +120,7 @@ __device__ __forceinline__ void next_unit(const PagedAttnParams& p, int items, C
   c.item = 0;
   do {
     if (++c.b >= p.c.n_seqs) { c.b = p.c.n_seqs - 1; return; }               // (behind the line's end: never used)
-    c.n = clamp_len<KT>(p, c.b);
+    c.n = clamp_len(p, c.b);
   } while (c.n < 0);
   c.tiles = tiles_of<KT>(c.n);
 }
@@ -140,6 +148,15 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1,
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+template <bool F16>      // without an accumulator
+__device__ __forceinline__ void mma_first(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  if (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ unsigned pack_h2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
@@ -161,22 +178,22 @@ __device__ __forceinline__ unsigned e4m3x2_to_h2(unsigned v) {
   return *reinterpret_cast<const unsigned*>(&h);
 }
 
-// Places of 16-byte chunks in a staged tile of 16 rows, such that neither the copies nor the loads below meet bank conflicts: keys are read by
-// (row r, chunk c mod 4) with two rows at a time, values by (rows 0, 2, 4, 6, neighbouring chunks).
+// Places of 16-byte chunks in a staged array of KT rows, such that neither the copies nor the loads below meet bank conflicts: keys are read by
+// (row, chunk c) with two neighbouring rows at a time, values by neighbouring chunks of four rows KT / 4 apart.
 template <int NCH> __device__ __forceinline__ int key_place(int row, int ch) { return NCH >= 8 ? row * NCH + (ch ^ ((row & 1) << 2)) : row * NCH + ch; }
-template <int NCH> __device__ __forceinline__ int value_place(int row, int ch) {
-  const int x = ((row >> 1) & 3) << 1;
+template <int NCH, int KT> __device__ __forceinline__ int value_place(int row, int ch) {
+  const int x = (row / (KT / 4) & 3) << 1;
   return NCH >= 8 ? row * NCH + (ch ^ x) : (row >> 1) * 8 + ((((row & 1) << 2) + ch) ^ x);
 }
 
 // ---- tensor-core consumer ------------------------------------------------------------------------
-// Lane (r = lane / 4, c = lane % 4) holds row (query head) r of scores and outputs: positions 8 t + 2 c + {0, 1} of score tile t, and DL = HD / 4
-// dimensions from DL' * c on (see dim()).
+// Lane (r = lane / 4, c = lane % 4) holds row (query head) r of scores and outputs.  Column n of score tile t is position (n / 2) * KT / 4 + 2 t + n % 2 of the
+// unit, so that a lane's KT / 4 positions are neighbours: c * KT / 4 + (0 .. KT / 4).
 template <typename CT, int HD, bool QF32>
 struct Mma {
   using S = Shape<CT, HD>;
   static constexpr bool F8 = sizeof(CT) == 1;
-  static constexpr int KS = HD / 16, NT = S::KT / 8, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
+  static constexpr int KS = HD / 16, NT = S::KT / 8, KPL = S::KT / 4, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
   unsigned q[TERMS][KS][2];
   float o[HD / 8][4];
   float m, l, mv, q_scale;                 // running maximum (log2 units), this lane's part of the sum, maximum of the scaled weights (F8)
@@ -246,59 +263,79 @@ struct Mma {
   // set in `bad`; the query is at position `at`.
   __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, int live, unsigned bad, int lane) {
     const int r = lane >> 2, c = lane & 3;
-    const bool slopes = p.q.alibi_slopes != nullptr;
     float s[NT][4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int i = 0; i < S::NCH / 4; ++i) {
+      unsigned x[NT][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
-      const uint4* kt = reinterpret_cast<const uint4*>(st + (t / 2) * 16 * S::RB);
-      const int row = (t & 1) * 8 + r;
+      for (int t = 0; t < NT; ++t) {
+        const uint4 w = reinterpret_cast<const uint4*>(st)[key_place<S::NCH>((r >> 1) * KPL + 2 * t + (r & 1), c + 4 * i)];
+        x[t][0] = w.x; x[t][1] = w.y; x[t][2] = w.z; x[t][3] = w.w;
+      }
+      constexpr int KC = E / 4, T1 = TERMS > 1 ? 1 : 0;        // contraction steps of a chunk; the tiles in turn, so that products do not wait for one another
 #pragma unroll
-      for (int i = 0; i < S::NCH / 4; ++i) {
-        const uint4 w = kt[key_place<S::NCH>(row, c + 4 * i)];
-        const unsigned x[4] = {w.x, w.y, w.z, w.w};
-        constexpr int KC = E / 4;          // contraction steps of a chunk
+      for (int u = 0; u < KC; ++u) {
+        const int k = i * KC + u;
+        const unsigned q2 = TERMS > 1 ? q[T1][k][0] : 0u, q3 = TERMS > 1 ? q[T1][k][1] : 0u;
 #pragma unroll
-        for (int u = 0; u < KC; ++u) {
-          const int k = i * KC + u;
-          unsigned b0, b1;
-          if (F8) { b0 = e4m3x2_to_h2(x[u]); b1 = e4m3x2_to_h2(x[u] >> 16); }
-          else { b0 = x[2 * u]; b1 = x[2 * u + 1]; }
-          const unsigned z = 0u;
-          if (F8) mma_f16(s[t], q[0][k][0], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][0] : z, q[0][k][1], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][1] : z, b0, b1);
-          else {
-            mma_bf16(s[t], q[0][k][0], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][0] : z, q[0][k][1], TERMS > 1 ? q[TERMS > 1 ? 1 : 0][k][1] : z, b0, b1);
-            if (TERMS > 2) mma_bf16(s[t], q[TERMS - 1][k][0], z, q[TERMS - 1][k][1], z, b0, b1);
-          }
+        for (int t = 0; t < NT; ++t) {
+          const unsigned b0 = F8 ? e4m3x2_to_h2(x[t][u]) : x[t][(2 * u) & 3], b1 = F8 ? e4m3x2_to_h2(x[t][u] >> 16) : x[t][(2 * u + 1) & 3];
+          if (k == 0) mma_first<F8>(s[t], q[0][k][0], q2, q[0][k][1], q3, b0, b1);
+          else if (F8) mma_f16(s[t], q[0][k][0], q2, q[0][k][1], q3, b0, b1);
+          else mma_bf16(s[t], q[0][k][0], q2, q[0][k][1], q3, b0, b1);
+        }
+        if (TERMS > 2) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_bf16(s[t], q[TERMS - 1][k][0], 0u, q[TERMS - 1][k][1], 0u, x[t][(2 * u) & 3], x[t][(2 * u + 1) & 3]);
         }
       }
     }
     // scores in log2 units (for F8 also those of the scaled weights), the maximum of the row, weights
     float a[NT][2], av[F8 ? NT : 1][2], top = m, topv = mv;
-    const float far = slopes ? (float)(j0 + 2 * c - at) : 0.f;
+    unsigned ke[KPL / 4], ve[KPL / 4];       // the exponents of this lane's positions
+    if (F8) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      unsigned kx = 0, vx = 0;
-      if (F8) {
-        kx = *reinterpret_cast<const uint16_t*>(st + S::KV + 8 * t + 2 * c);
-        vx = *reinterpret_cast<const uint16_t*>(st + S::KV + S::KT + 8 * t + 2 * c);
+      for (int y = 0; y < KPL / 4; ++y) {
+        ke[y] = reinterpret_cast<const unsigned*>(st + S::KV + KPL * c)[y];
+        ve[y] = reinterpret_cast<const unsigned*>(st + S::KV + S::KT + KPL * c)[y];
       }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
+        const int j = 2 * t + e;             // of the lane's positions
         float x = TERMS > 1 ? s[t][e] + s[t][e + 2] : s[t][e];
-        x *= F8 ? q_scale * __uint_as_float((e ? kx << 15 : kx << 23) & 0x7f800000u) : q_scale;
-        if (slopes) x = fmaf(slope, far + (float)(8 * t + e), x);
+        if (F8) {
+          const unsigned kw = ke[j / 4], b = j % 4;
+          x *= q_scale * __uint_as_float(b == 3 ? kw >> 1 & 0x7f800000u : kw << (23 - 8 * b) & 0x7f800000u);
+        } else {
+          x *= q_scale;
+        }
         a[t][e] = x;
-        if (F8) av[F8 ? t : 0][e] = x + (__uint_as_float(__byte_perm(vx, 0x4b000000u, e ? 0x7551u : 0x7550u)) - 8388735.f);     // 2^23 + exponent - (2^23 + 127)
       }
+    if (p.q.alibi_slopes) {
+      const float far = (float)(j0 + KPL * c - at);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) a[t][e] = fmaf(slope, far + (float)(2 * t + e), a[t][e]);
+    }
+    if (F8) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {        // 2^23 + exponent - (2^23 + 127)
+          const int j = 2 * t + e;
+          av[F8 ? t : 0][e] = a[t][e] + (__uint_as_float(__byte_perm(ve[j / 4], 0x4b000000u, 0x7550u + j % 4)) - 8388735.f);
+        }
     }
     if (live < S::KT || bad) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (8 * t + 2 * c + e >= live || (bad >> (t / 2) & 1)) {
+          if (KPL * c + 2 * t + e >= live || (bad >> ((KPL * c) / 16) & 1)) {
             a[t][e] = -INFINITY;
             if (F8) av[F8 ? t : 0][e] = -INFINITY;
           }
@@ -330,7 +367,7 @@ struct Mma {
     const float ref = m == -INFINITY ? 0.f : m, refv = mv == -INFINITY ? 0.f : mv - kWeightLog2;
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
-      float w[4];                          // positions 2c, 2c + 1, 8 + 2c, 9 + 2c of the sixteen
+      float w[4];                          // positions 4 sub + (0 .. 3) of the lane's
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int t = 2 * sub + e / 2;
@@ -347,25 +384,34 @@ struct Mma {
           w2[h] = pack2(w[2 * h], w[2 * h + 1]);
         }
       }
-      const unsigned char* vt = st + S::KT * S::RB + sub * 16 * S::RB;
-      const int rows[4] = {2 * c, 2 * c + 1, 8 + 2 * c, 9 + 2 * c};
+      const unsigned char* vt = st + S::KT * S::RB;
+      const int row0 = KPL * c + 4 * sub;
       if (!F8) {
 #pragma unroll
         for (int i = 0; i < S::NCH / 8; ++i) {         // chunk r + 8 i of the four rows: dimensions 64 i + 8 r + (0 .. 7)
           unsigned x[4][4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH>(rows[k], r + 8 * i)];
+            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH, S::KT>(row0 + k, r + 8 * i)];
             x[k][0] = y.x; x[k][1] = y.y; x[k][2] = y.z; x[k][3] = y.w;
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
-            const unsigned b0 = __byte_perm(x[0][j / 2], x[1][j / 2], sel), b1 = __byte_perm(x[2][j / 2], x[3][j / 2], sel);
-            Out acc(o[8 * i + j]);
-            mma_bf16(acc.c, w0[0], w1[0], w0[1], w1[1], b0, b1);
-            mma_bf16(acc.c, w2[0], 0u, w2[1], 0u, b0, b1);
-            acc.add(o[8 * i + j]);
+          for (int half = 0; half < 2; ++half) {       // four products, then the four of the third term
+            Out acc[4] = {o[8 * i + 4 * half], o[8 * i + 4 * half + 1], o[8 * i + 4 * half + 2], o[8 * i + 4 * half + 3]};
+            unsigned b0[4], b1[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int j = 4 * half + y;
+              const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
+              b0[y] = __byte_perm(x[0][j / 2], x[1][j / 2], sel);
+              b1[y] = __byte_perm(x[2][j / 2], x[3][j / 2], sel);
+              mma_bf16(acc[y].c, w0[0], w1[0], w0[1], w1[1], b0[y], b1[y]);
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              mma_bf16(acc[y].c, w2[0], 0u, w2[1], 0u, b0[y], b1[y]);
+              acc[y].add(o[8 * i + 4 * half + y]);
+            }
           }
         }
       } else {
@@ -374,10 +420,10 @@ struct Mma {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if constexpr (WD == 2) {
-            const uint2 y = *reinterpret_cast<const uint2*>(vt + value_place<S::NCH>(rows[k], r >> 1) * 16 + (r & 1) * 8);
+            const uint2 y = *reinterpret_cast<const uint2*>(vt + value_place<S::NCH, S::KT>(row0 + k, r >> 1) * 16 + (r & 1) * 8);
             x[k][0] = y.x; x[k][1] = y.y;
           } else {
-            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH>(rows[k], r)];
+            const uint4 y = reinterpret_cast<const uint4*>(vt)[value_place<S::NCH, S::KT>(row0 + k, r)];
             x[k][0] = y.x; x[k][1] = y.y; x[k][2] = y.z; x[k][3] = y.w;
           }
         }
@@ -452,7 +498,7 @@ struct Simt {
       const int j = i * KPI + sub;
       const bool ok = j < live && !bad;
       const float4 k = reinterpret_cast<const float4*>(st)[key_place<S::NCH>(j, c)];
-      const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH>(j, c)];
+      const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH, S::KT>(j, c)];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         float a = q[g][0] * k.x + q[g][1] * k.y + q[g][2] * k.z + q[g][3] * k.w;
@@ -524,27 +570,39 @@ __device__ __noinline__ void slow_piece(const PagedAttnParams& p, int b, int kvh
 }
 
 // ---- what both kernels end with: the own pair, the division, out and lse ---------------------------
-// A warp finishes query head h of sequence b: m, l and this lane's dimensions d * 32 + lane of o.
+// The own pair of query head h of sequence b, as its warp holds it: the score and this lane's dimensions d * 32 + lane of the value.
 template <int HD>
-__device__ __forceinline__ void finish_head(const PagedAttnParams& p, int b, int h, int lane, float m, float l, float (&o)[HD / 32]) {
-  const int kvh = h / p.group;
-  if (p.q.k_own) {
-    float a = 0.f;
+struct Own {
+  float a, v[HD / 32];
+  __device__ __forceinline__ void load(const PagedAttnParams& p, int b, int h, int lane) {
+    a = -INFINITY;
 #pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-      a += q_at(p.q.dtype, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + d * 32 + lane) *
-           q_at(p.q.dtype, p.q.k_own, (size_t)b * p.q.k_own_stride + (size_t)kvh * HD + d * 32 + lane);
-    a = warp_sum(a) * p.scale_log2;
-    const float mn = fmaxf(m, a), ref = mn == -INFINITY ? 0.f : mn, w0 = exp2f(m - ref), w1 = exp2f(a - ref);
+    for (int d = 0; d < HD / 32; ++d) v[d] = 0.f;
+    if (!p.q.k_own) return;
+    const size_t qa = (size_t)b * p.q.q_stride + (size_t)h * HD, kvh = (size_t)(h / p.group) * HD;
+    float x = 0.f;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+      x += q_at(p.q.dtype, p.q.q, qa + d * 32 + lane) * q_at(p.q.dtype, p.q.k_own, (size_t)b * p.q.k_own_stride + kvh + d * 32 + lane);
+      v[d] = q_at(p.q.dtype, p.q.v_own, (size_t)b * p.q.v_own_stride + kvh + d * 32 + lane);
+    }
+    a = warp_sum(x) * p.scale_log2;
+  }
+};
+// m, l and this lane's dimensions of o over the cached pairs -> out, lse
+template <int HD>
+__device__ __forceinline__ void finish_head(const PagedAttnParams& p, const Own<HD>& own, int b, int h, int lane, float m, float l, float (&o)[HD / 32]) {
+  if (p.q.k_own) {
+    const float mn = fmaxf(m, own.a), ref = mn == -INFINITY ? 0.f : mn, w0 = ex2(m - ref), w1 = ex2(own.a - ref);
     m = mn;
     l = l * w0 + w1;
 #pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-      o[d] = o[d] * w0 + w1 * q_at(p.q.dtype, p.q.v_own, (size_t)b * p.q.v_own_stride + (size_t)kvh * HD + d * 32 + lane);
+    for (int d = 0; d < HD / 32; ++d) o[d] = o[d] * w0 + w1 * own.v[d];
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) {
-    const float y = l == 0.f ? 0.f : o[d] / l;
+    const float y = l == 0.f ? 0.f : o[d] * inv;
     const size_t i = (size_t)b * p.q.out_stride + (size_t)h * HD + d * 32 + lane;
     if (p.q.dtype == RT_BF16) ((__nv_bfloat16*)p.q.out)[i] = __float2bfloat16_rn(y);
     else ((float*)p.q.out)[i] = y;
@@ -560,19 +618,18 @@ template <typename CT, int HD, typename Consumer>
 __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_kernel(const __grid_constant__ PagedAttnParams p, float* part, int part_rows) {
   using S = Shape<CT, HD>;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ long long sums[kWarps * 32], warp_sums[kWarps];
+  __shared__ unsigned sums[kWarps * 32], warp_sums[kWarps];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (p.group + kRows - 1) / kRows, items = p.c.n_kv_heads * slices;
-  const Line ln = scan_line<S::KT, kWarps * 32>(p, items, sums, warp_sums, blockIdx.x == 0);
-  const long long workers = workers_of(ln.total, S::WORKERS);
-  const long long me = (long long)warp * gridDim.x + blockIdx.x;               // neighbours on the line sit on different SMs
-  if (me >= workers) return;
-  const long long u0 = ln.total * me / workers;
-  const int count = (int)(ln.total * (me + 1) / workers - u0);
+  const Line ln = scan_line<S::KT, kWarps * 32>(p, items, S::WORKERS, sums, warp_sums, blockIdx.x == 0);
+  const unsigned me = warp * gridDim.x + blockIdx.x;                           // neighbours on the line sit on different SMs
+  if (me >= ln.workers) return;
+  const unsigned u0 = ln.begin(me);
+  const int count = (int)(ln.begin(me + 1) - u0);
 
   // where the line stands at u0
-  Cursor cp;
+  Cursor cc;
   {
     int lo = 0, hi = kWarps * 32 - 1;
     while (lo < hi) {
@@ -580,101 +637,122 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
       if (sums[mid] <= u0) lo = mid; else hi = mid - 1;
     }
     // (several threads may hold no sequence: the last one whose sum is <= u0 has the unit, or begins behind sequences without units)
-    long long rest = u0 - sums[lo];
+    unsigned rest = u0 - sums[lo];
     int b = lo * ln.per;
     for (;; ++b) {
-      cp.n = clamp_len<S::KT>(p, b);
-      cp.tiles = tiles_of<S::KT>(cp.n);
-      const long long here = (long long)cp.tiles * items;
+      cc.n = clamp_len(p, b);
+      cc.tiles = tiles_of<S::KT>(cc.n);
+      const unsigned here = (unsigned)cc.tiles * items;
       if (rest < here) break;
       rest -= here;
     }
-    cp.b = b;
-    cp.item = (int)(rest / cp.tiles);
-    cp.tile = (int)(rest % cp.tiles);
+    cc.b = b;
+    cc.item = (int)(rest / (unsigned)cc.tiles);
+    cc.tile = (int)(rest - (unsigned)cc.item * cc.tiles);
   }
-  Cursor cc = cp;
 
+  // The producer: its cursor, and what changes with the head only.  The table is looked up a unit ahead of the copies.
+  Cursor cp = cc;
   unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
   const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
-  int pages[S::SUB], kvh = head_of(cp.item, slices);
-  unsigned bad = 0;                                                            // SUB bits a stage: pages that do not exist
-  auto fetch_pages = [&]() {                                                   // of the producer's unit
+  const unsigned page_bytes = (unsigned)p.c.n_kv_heads * p.c.page_size * S::RB;
+  const int in_page = p.c.page_size - 1, log_page = p.log_page;
+  const unsigned n_pages = p.c.n_pages;
+  const int* table;
+  const unsigned char *k0, *v0;                                                // this lane's first chunk of the head in page 0
+  const uint8_t* e0;                                                           // lanes 0 .. 2 SUB - 1: exponents of keys (even), values (odd) of a sixteen
+  unsigned bad = 0;                                                            // SUB bits a stage: sixteens without a page
+  auto enter_head = [&]() {
+    const size_t kv_row = (size_t)head_of(cp.item, slices) * p.c.page_size;
+    table = p.c.page_table + (size_t)cp.b * p.c.max_pages;
+    k0 = (const unsigned char*)p.c.k + kv_row * S::RB + lane * 16;
+    v0 = (const unsigned char*)p.c.v + kv_row * S::RB + lane * 16;
+    e0 = ((lane & 1) ? p.c.v_exp : p.c.k_exp) + kv_row;
+  };
+  int pages[S::SUB];
+  auto fetch_pages = [&]() {
+    const int j = cp.tile * S::KT;
 #pragma unroll
-    for (int s = 0; s < S::SUB; ++s) {
-      const int j = cp.tile * S::KT + 16 * s;
-      pages[s] = j < cp.n ? __ldg(p.c.page_table + (size_t)cp.b * p.c.max_pages + (j >> p.log_page)) : -1;
-    }
+    for (int s = 0; s < S::SUB; ++s) pages[s] = j + 16 * s < cp.n ? __ldg(table + ((j + 16 * s) >> log_page)) : -1;
   };
   auto produce = [&](int stage) {
     const unsigned dst = ring_at + stage * S::STAGE;
-    bad &= ~(((1u << S::SUB) - 1) << (stage * S::SUB));
+    const int j = cp.tile * S::KT;
+    bool full = j + S::KT <= cp.n;
 #pragma unroll
-    for (int s = 0; s < S::SUB; ++s) {
-      const int j = cp.tile * S::KT + 16 * s;
-      const bool ok = (unsigned)pages[s] < (unsigned)p.c.n_pages;
-      const size_t row = ((size_t)(ok ? pages[s] : 0) * p.c.n_kv_heads + kvh) * p.c.page_size + (j & (p.c.page_size - 1));
-      const unsigned char* k = (const unsigned char*)p.c.k + row * S::RB + lane * 16;
-      const unsigned char* v = (const unsigned char*)p.c.v + row * S::RB + lane * 16;
-      const unsigned kd = dst + s * 16 * S::RB, vd = kd + S::KT * S::RB;
-      if (ok && j + 16 <= cp.n) {
+    for (int s = 0; s < S::SUB; ++s) full = full && (unsigned)pages[s] < n_pages;
+    bad &= ~(((1u << S::SUB) - 1) << (stage * S::SUB));
+    if (full) {
+      size_t off[S::SUB];
+#pragma unroll
+      for (int s = 0; s < S::SUB; ++s) {
+        off[s] = (size_t)pages[s] * page_bytes + (unsigned)(((j + 16 * s) & in_page) * S::RB);
+        const unsigned char *k = k0 + off[s], *v = v0 + off[s];
 #pragma unroll
         for (int i = 0; i < S::NCH / 2; ++i) {
-          const int row_in = 32 / S::NCH * i + lane / S::NCH, ch = lane % S::NCH;
-          copy16(kd + key_place<S::NCH>(row_in, ch) * 16, k + i * 512, 16);
-          copy16(vd + value_place<S::NCH>(row_in, ch) * 16, v + i * 512, 16);
+          const int row = 16 * s + 32 / S::NCH * i + lane / S::NCH, ch = lane % S::NCH;
+          copy16(dst + key_place<S::NCH>(row, ch) * 16, k + i * 512, 16);
+          copy16(dst + S::KT * S::RB + value_place<S::NCH, S::KT>(row, ch) * 16, v + i * 512, 16);
         }
-      } else {
-        const int live = ok ? cp.n - j : 0;
+      }
+      if (S::EXP && lane < 2 * S::SUB)
+        copy16(dst + S::KV + (lane & 1) * S::KT + (lane >> 1) * 16, e0 + (S::SUB > 1 && lane > 1 ? off[S::SUB - 1] : off[0]) / S::RB, 16);
+    } else {
+#pragma unroll 1
+      for (int s = 0; s < S::SUB; ++s) {
+        const int page = s ? pages[S::SUB - 1] : pages[0], js = j + 16 * s;
+        const bool ok = (unsigned)page < n_pages;
+        const int live = ok ? cp.n - js : 0;
+        const size_t off = ok ? (size_t)page * page_bytes + (unsigned)((js & in_page) * S::RB) : 0;
         if (!ok) {
           bad |= 1u << (stage * S::SUB + s);
-          if (j < cp.n && p.c.status && lane == 0) *p.c.status = RT_ERR_INVALID_ARG;
+          if (js < cp.n && p.c.status && lane == 0) *p.c.status = RT_ERR_INVALID_ARG;
         }
 #pragma unroll 1
         for (int i = 0; i < S::NCH / 2; ++i) {
-          const int row_in = (i * 32 + lane) / S::NCH, ch = lane % S::NCH;
-          const bool in = row_in < live;
-          copy16(kd + key_place<S::NCH>(row_in, ch) * 16, in ? k + i * 512 : (const unsigned char*)p.c.k, in ? 16 : 0);
-          copy16(vd + value_place<S::NCH>(row_in, ch) * 16, in ? v + i * 512 : (const unsigned char*)p.c.v, in ? 16 : 0);
+          const int row = (i * 32 + lane) / S::NCH, ch = lane % S::NCH;
+          const bool in = row < live;
+          copy16(dst + key_place<S::NCH>(16 * s + row, ch) * 16, in ? k0 + off + i * 512 : (const unsigned char*)p.c.k, in ? 16 : 0);
+          copy16(dst + S::KT * S::RB + value_place<S::NCH, S::KT>(16 * s + row, ch) * 16, in ? v0 + off + i * 512 : (const unsigned char*)p.c.v, in ? 16 : 0);
         }
-      }
-      if (S::EXP && lane < 2) {
-        const uint8_t* e = lane ? p.c.v_exp : p.c.k_exp;
-        copy16(dst + S::KV + lane * S::KT + 16 * s, ok ? e + row : e, ok ? 16 : 0);
+        if (S::EXP && lane < 2) copy16(dst + S::KV + lane * S::KT + 16 * s, ok ? e0 + off / S::RB : (const uint8_t*)p.c.k, ok ? 16 : 0);
       }
     }
-  };
-  auto advance = [&]() {
-    const int before = cp.item;
-    next_unit<S::KT>(p, items, cp);
-    if (cp.item != before) kvh = head_of(cp.item, slices);
+    if (++cp.tile == cp.tiles) {
+      --cp.tile;
+      next_unit<S::KT>(p, items, cp);
+      enter_head();
+    }
   };
 
   Consumer con;
+  enter_head();
   fetch_pages();
 #pragma unroll
   for (int s = 0; s < S::STAGES - 1; ++s) {
     if (s < count) {
       produce(s);
-      advance();
-      if (s + 1 < count) fetch_pages();
+      fetch_pages();
     }
     copy_commit();
   }
-  bool fresh = true;
+  auto begin_head = [&]() {
+    const int g0 = (slices == 1 ? 0 : cc.item % slices) * kRows;
+    con.begin(p, cc.b, head_of(cc.item, slices) * p.group + g0, min(kRows, p.group - g0), lane);
+  };
+  begin_head();                                                                // (the first head's queries arrive beside its pairs)
+  bool fresh = false;
   int first_tile = cc.tile, stage = 0;
   for (int i = 0; i < count; ++i, stage = stage + 1 == S::STAGES ? 0 : stage + 1) {
     copy_wait<S::STAGES - 2>();
     __syncwarp();
     if (i + S::STAGES - 1 < count) {
       produce(stage == 0 ? S::STAGES - 1 : stage - 1);
-      advance();
-      if (i + S::STAGES < count) fetch_pages();
+      fetch_pages();
     }
     copy_commit();
     if (fresh) {
-      const int g0 = (slices == 1 ? 0 : cc.item % slices) * kRows;
-      con.begin(p, cc.b, head_of(cc.item, slices) * p.group + g0, min(kRows, p.group - g0), lane);
+      begin_head();
       first_tile = cc.tile;
       fresh = false;
     }
@@ -696,9 +774,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
       if (ends && first_tile == 0) {
         for (int g = 0; g < g_in; ++g) {
           float x[HD / 32];
+          Own<HD> own;
+          own.load(p, cc.b, h0 + g, lane);
 #pragma unroll
           for (int d = 0; d < HD / 32; ++d) x[d] = out[g * HD + d * 32 + lane];
-          finish_head<HD>(p, cc.b, h0 + g, lane, out[kRows * HD + 2 * g], out[kRows * HD + 2 * g + 1], x);
+          finish_head<HD>(p, own, cc.b, h0 + g, lane, out[kRows * HD + 2 * g], out[kRows * HD + 2 * g + 1], x);
         }
       } else {
         float* slot = part + ((size_t)me * 2 + (first_tile == 0 ? 1 : 0)) * slot_floats(part_rows, HD);
@@ -709,42 +789,48 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
         if (lane < 2 * g_in) slot[part_rows * HD + lane] = out[kRows * HD + lane];
       }
       fresh = true;
+      next_unit<S::KT>(p, items, cc);
+    } else {
+      ++cc.tile;
     }
-    next_unit<S::KT>(p, items, cc);
   }
 }
 
-// Joins the heads that several warps of the kernel above share: a block takes a query head, its warps every kJoinWarps-th partial result.
+// Joins the heads that several warps of the kernel above share: a block takes a query head, its warps every kJoinWarps-th partial result.  It
+// starts beside that kernel (programmatic launch): all that does not depend on its results is done before the wait.
 constexpr int kJoinWarps = 8;
 template <int KT, int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __grid_constant__ PagedAttnParams p, const float* part, int part_rows, int max_workers) {
-  __shared__ long long sums[kJoinWarps * 32], warp_sums[kJoinWarps];
+  __shared__ unsigned sums[kJoinWarps * 32], warp_sums[kJoinWarps];
   __shared__ float sm_o[kJoinWarps][HD], sm_m[kJoinWarps], sm_l[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (p.group + kRows - 1) / kRows, items = p.c.n_kv_heads * slices;
-  const Line ln = scan_line<KT, kJoinWarps * 32>(p, items, sums, warp_sums, false);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (ln.total == 0) return;
-  const long long workers = workers_of(ln.total, max_workers);
-  const long long all = (long long)p.c.n_seqs * p.q.n_heads;
+  const Line ln = scan_line<KT, kJoinWarps * 32>(p, items, max_workers, sums, warp_sums, false);
+  bool waited = false;
+  const long long all = ln.total ? (long long)p.c.n_seqs * p.q.n_heads : 0;
   for (long long x = blockIdx.x; x < all; x += gridDim.x) {
-    const int b = (int)(x / p.q.n_heads), h = (int)(x % p.q.n_heads);
-    const int n = clamp_len<KT>(p, b);
+    const int b = (int)(x / p.q.n_heads), h = (int)(x - (long long)b * p.q.n_heads);
+    const int n = clamp_len(p, b);
     if (n < 0) continue;
-    long long u = sums[b / ln.per];
-    for (int s = b / ln.per * ln.per; s < b; ++s) u += (long long)tiles_of<KT>(clamp_len<KT>(p, s)) * items;
+    unsigned u = sums[b / ln.per];
+    for (int s = b / ln.per * ln.per; s < b; ++s) u += (unsigned)tiles_of<KT>(clamp_len(p, s)) * items;
     const int tiles = tiles_of<KT>(n), g = h % p.group;
-    u += (long long)(h / p.group * slices + g / kRows) * tiles;
-    const long long w0 = worker_of(u, ln.total, workers), w1 = worker_of(u + tiles - 1, ln.total, workers);
+    u += (unsigned)(h / p.group * slices + g / kRows) * tiles;
+    const unsigned w0 = ln.worker_of(u), w1 = ln.worker_of(u + tiles - 1);
     if (w0 == w1) continue;                                            // written by the warp that held all of it
     const int r = g % kRows;
+    Own<HD> own;
+    if (warp == 0) own.load(p, b, h, lane);
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+    waited = true;
     float m = -INFINITY, l = 0.f, o[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
-    for (long long w = w0 + warp; w <= w1; w += kJoinWarps) {
+#pragma unroll 2
+    for (unsigned w = w0 + warp; w <= w1; w += kJoinWarps) {
       const float* slot = part + ((size_t)w * 2 + (w == w0 ? 1 : 0)) * slot_floats(part_rows, HD);
       const float ms = slot[part_rows * HD + 2 * r], ls = slot[part_rows * HD + 2 * r + 1];
-      const float mn = fmaxf(m, ms), ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref), f1 = exp2f(ms - ref);
+      const float mn = fmaxf(m, ms), ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(m - ref), f1 = ex2(ms - ref);
       m = mn;
       l = l * f0 + ls * f1;
 #pragma unroll
@@ -764,14 +850,15 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __gri
       for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
 #pragma unroll
       for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = exp2f(sm_m[w] - ref);
+        const float f = ex2(sm_m[w] - ref);
         la += sm_l[w] * f;
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) o[d] += sm_o[w][d * 32 + lane] * f;
       }
-      finish_head<HD>(p, b, h, lane, ma, la, o);
+      finish_head<HD>(p, own, b, h, lane, ma, la, o);
     }
   }
+  if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");      // (this grid must not end before the one it follows)
 }
 
 int part_rows_of(int group) { return group < kRows ? group : kRows; }
@@ -792,6 +879,7 @@ cudaError_t launch_split(const PagedAttnParams& p, float* part, cudaStream_t s) 
   const long long slices = ceil_div(p.group, kRows);
   const long long most = (long long)p.c.n_seqs * p.c.n_kv_heads * slices * max(1LL, ((long long)p.c.max_pages * p.c.page_size + S::KT - 1) / S::KT);
   const int grid = (int)(most < kSms * S::CTAS ? most : kSms * S::CTAS);
+  if (most > 0x7fffffffLL) return cudaErrorInvalidValue;            // (paged_attn_counts refuses these)
   kernel<<<grid, kWarps * 32, S::SMEM, s>>>(p, part, part_rows_of(p.group));
   const cudaError_t e1 = cudaGetLastError();
   if (e1 != cudaSuccess || most <= (long long)p.c.n_seqs * p.c.n_kv_heads * slices) return e1;
@@ -813,6 +901,11 @@ cudaError_t launch_simt(const PagedAttnParams& p, float* part, cudaStream_t s) {
 }
 
 }  // namespace
+
+bool paged_attn_counts(const rt_paged_cache* c, int n_heads) {
+  const long long items = (long long)c->n_kv_heads * ceil_div(n_heads / c->n_kv_heads, kRows), units = (long long)c->max_pages * (c->page_size / 16);
+  return units <= 0x7fffffffLL / items / c->n_seqs && (long long)c->max_pages * c->page_size <= 0x7fffffffLL;
+}
 
 size_t paged_attn_workspace(const rt_paged_cache* c, int n_heads) {
   const int hd = c->head_dim, rows = part_rows_of(n_heads / c->n_kv_heads);

@@ -326,23 +326,23 @@ def _raw_stream(index: int) -> int:
     return _torch()._C._cuda_getCurrentRawStream(index)
 
 
-def _rows(t, heads: int, head_dim: int, n: int, dtype, device, where: str) -> tuple:
-    """(address, stride) of [n, heads, head_dim] or [n, heads * head_dim] rows whose heads are contiguous."""
+def _rows(t, heads: int, head_dim: int, n: int, dtype, index: int, where: str) -> tuple:
+    """(address, stride) of [n, heads, head_dim] or [n, heads * head_dim] rows on CUDA device `index` whose heads are contiguous."""
     st, sh = t.stride(), t.shape
     if len(sh) == 3:
         ok = sh[1] == heads and sh[2] == head_dim and st[2] == 1 and (heads == 1 or st[1] == head_dim)
     else:
         ok = len(sh) == 2 and sh[1] == heads * head_dim and st[1] == 1
-    if not ok or sh[0] != n or t.dtype != dtype or t.device != device:
+    if not ok or sh[0] != n or t.dtype != dtype or t.get_device() != index:
         raise RtError(RT_ERR_INVALID_ARG, where)
     return t.data_ptr(), st[0]
 
 
-def _vector(t, n: int, dtype, device, where: str):
-    """Address of a contiguous array of n elements, None for None."""
+def _vector(t, n: int, dtype, index: int, where: str):
+    """Address of a contiguous array of n elements on CUDA device `index`, None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+    if t.dtype != dtype or t.numel() != n or t.get_device() != index or not t.is_contiguous():
         raise RtError(RT_ERR_INVALID_ARG, where)
     return t.data_ptr()
 
@@ -596,23 +596,22 @@ class PagedCache:
 
     def __init__(self, k, v, page_table, k_exp=None, v_exp=None):
         torch = _torch()
-        where = "PagedCache"
         self.device, self.k, self.v, self.page_table, self.k_exp, self.v_exp = k.device, k, v, page_table, k_exp, v_exp
         code = {torch.float32: RT_F32, torch.bfloat16: RT_BF16, torch.float8_e4m3fn: RT_E4M3}.get(k.dtype)
         _require(k.is_cuda and code is not None and k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and v.device == k.device and
-                 k.is_contiguous() and v.is_contiguous(), where + ": k, v")
+                 k.is_contiguous() and v.is_contiguous(), "PagedCache: k, v")
         _require(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.device == k.device,
-                 where + ": page_table")
+                 "PagedCache: page_table")
         n_pages, n_kv, page, hd = k.shape
-        _require((k_exp is not None) == (code == RT_E4M3) and (v_exp is not None) == (code == RT_E4M3), where + ": exponents")
+        _require((k_exp is not None) == (code == RT_E4M3) and (v_exp is not None) == (code == RT_E4M3), "PagedCache: exponents")
         self._status = torch.zeros(1, dtype=torch.int32, device=k.device)
-        self._c = RtPagedCache(k.data_ptr(), v.data_ptr(), _vector(k_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": k_exp"),
-                               _vector(v_exp, n_pages * n_kv * page, torch.uint8, k.device, where + ": v_exp"), page_table.data_ptr(),
+        self._c = RtPagedCache(k.data_ptr(), v.data_ptr(), _vector(k_exp, n_pages * n_kv * page, torch.uint8, k.device.index, "PagedCache: k_exp"),
+                               _vector(v_exp, n_pages * n_kv * page, torch.uint8, k.device.index, "PagedCache: v_exp"), page_table.data_ptr(),
                                self._status.data_ptr(), n_pages, page, n_kv, hd, code, page_table.shape[0], page_table.shape[1])
         self._index = k.device.index
         self._codes = {torch.float32: RT_F32, torch.bfloat16: RT_BF16}
-        self._need: dict = {}                          # workspace bytes by number of query heads
-        _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, where + ": shape")
+        self._ws_like: dict = {}                       # by number of query heads: one word seen as an array of the workspace's size
+        _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, "PagedCache: shape")
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, n_seqs: int, max_pages: int, head_dim: int = 64, dtype: str = "bf16",
@@ -628,32 +627,31 @@ class PagedCache:
     def write(self, k, v, seq, pos) -> None:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
         seq[r] (int32); a negative position skips the row."""
-        torch, c, n = _torch(), self._c, k.shape[0]
-        if torch.cuda.current_device() != self._index:
-            with torch.cuda.device(self._index):
+        torch, c, dev, n = _torch(), self._c, self._index, k.shape[0]
+        if torch.cuda.current_device() != dev:
+            with torch.cuda.device(dev):
                 return self.write(k, v, seq, pos)
-        where = "PagedCache.write"
-        _require(k.dtype in self._codes, where + ": k")
-        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": k")
-        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, k.dtype, self.device, where + ": v")
-        sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
-        _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, _raw_stream(self._index)), "rt_cache_write")
+        _require(k.dtype in self._codes, "PagedCache.write: k")
+        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, k.dtype, dev, "PagedCache.write: k")
+        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, k.dtype, dev, "PagedCache.write: v")
+        sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.write: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.write: pos")
+        _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, _raw_stream(dev)), "rt_cache_write")
 
     def read(self, seq, pos, dtype: str = "bf16", k=None, v=None):
         """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
         Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
-        torch, c, n = _torch(), self._c, pos.shape[0]
-        if torch.cuda.current_device() != self._index:
-            with torch.cuda.device(self._index):
+        torch, c, dev, n = _torch(), self._c, self._index, pos.shape[0]
+        if torch.cuda.current_device() != dev:
+            with torch.cuda.device(dev):
                 return self.read(seq, pos, dtype, k, v)
-        where, t = "PagedCache.read", _tdtype(dtype)
+        t = _tdtype(dtype)
         shape = (n, c.n_kv_heads, c.head_dim)
         k = torch.empty(shape, dtype=t, device=self.device) if k is None else k
         v = torch.empty(shape, dtype=t, device=self.device) if v is None else v
-        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": k")
-        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, self.device, where + ": v")
-        sp, pp = _vector(seq, n, torch.int32, self.device, where + ": seq"), _vector(pos, n, torch.int32, self.device, where + ": pos")
-        _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, _raw_stream(self._index)), "rt_cache_read")
+        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: k")
+        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: v")
+        sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.read: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.read: pos")
+        _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, _raw_stream(dev)), "rt_cache_read")
         return k, v
 
     def attend(self, q, lens, k_own=None, v_own=None, scale: Optional[float] = None, alibi_slopes=None, out=None, lse=None):
@@ -661,31 +659,33 @@ class PagedCache:
         if given, to its own pair k_own, v_own [n_seqs, n_kv_heads, head_dim] -> out [n_seqs, n_heads, head_dim].  lse (float32
         [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
         whatever the memory holds)."""
-        torch, c = _torch(), self._c
-        if torch.cuda.current_device() != self._index:
-            with torch.cuda.device(self._index):
+        torch, c, dev = _torch(), self._c, self._index
+        if torch.cuda.current_device() != dev:
+            with torch.cuda.device(dev):
                 return self.attend(q, lens, k_own, v_own, scale, alibi_slopes, out, lse)
-        where, B, hd = "PagedCache.attend", c.n_seqs, c.head_dim
-        _require(q.dtype in self._codes and q.dim() == 3, where + ": q")
+        B, kv, hd = c.n_seqs, c.n_kv_heads, c.head_dim
+        _require(q.dtype in self._codes and q.dim() == 3, "PagedCache.attend: q")
         H, t = q.shape[1], q.dtype
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         a = RtPagedQuery()
-        a.q, a.q_stride = _rows(q, H, hd, B, t, self.device, where + ": q")
-        a.out, a.out_stride = _rows(out, H, hd, B, t, self.device, where + ": out")
-        _require((k_own is None) == (v_own is None), where + ": k_own, v_own")
+        a.q, a.q_stride = _rows(q, H, hd, B, t, dev, "PagedCache.attend: q")
+        a.out, a.out_stride = _rows(out, H, hd, B, t, dev, "PagedCache.attend: out")
+        _require((k_own is None) == (v_own is None), "PagedCache.attend: k_own, v_own")
         if k_own is not None:
-            a.k_own, a.k_own_stride = _rows(k_own, c.n_kv_heads, hd, B, t, self.device, where + ": k_own")
-            a.v_own, a.v_own_stride = _rows(v_own, c.n_kv_heads, hd, B, t, self.device, where + ": v_own")
-        a.lens = _vector(lens, B, torch.int32, self.device, where + ": lens")
-        a.alibi_slopes = _vector(alibi_slopes, H, torch.float32, self.device, where + ": alibi_slopes")
-        a.lse = _vector(lse, B * H, torch.float32, self.device, where + ": lse")
+            a.k_own, a.k_own_stride = _rows(k_own, kv, hd, B, t, dev, "PagedCache.attend: k_own")
+            a.v_own, a.v_own_stride = _rows(v_own, kv, hd, B, t, dev, "PagedCache.attend: v_own")
+        a.lens = _vector(lens, B, torch.int32, dev, "PagedCache.attend: lens")
+        a.alibi_slopes = _vector(alibi_slopes, H, torch.float32, dev, "PagedCache.attend: alibi_slopes")
+        a.lse = _vector(lse, B * H, torch.float32, dev, "PagedCache.attend: lse")
         a.dtype, a.n_heads, a.softmax_scale = self._codes[t], H, 1.0 / math.sqrt(hd) if scale is None else scale
-        need = self._need.get(H)
-        if need is None:
-            need = self._need[H] = rt_paged_attention_workspace_bytes(c, H)
-            _require(need > 0, where + ": q")
-        ws = torch.empty(need, dtype=torch.uint8, device=self.device)       # of its own for every call: calls on two streams may overlap
-        _check(rt_paged_attention(c, a, ws.data_ptr(), need, _raw_stream(self._index)), "rt_paged_attention")
+        like = self._ws_like.get(H)
+        if like is None:
+            need = rt_paged_attention_workspace_bytes(c, H)
+            _require(need > 0, "PagedCache.attend: q")
+            like = self._ws_like[H] = self._status.expand(need // 4)
+        # a workspace of its own for every call: calls on two streams, or two captured graphs, may overlap
+        ws = torch.empty_like(like, memory_format=torch.contiguous_format)
+        _check(rt_paged_attention(c, a, ws.data_ptr(), 4 * ws.numel(), _raw_stream(dev)), "rt_paged_attention")
         return out
 
     def status(self) -> int:
@@ -710,50 +710,50 @@ class QkRotate:
                                   rot_dim, {"halves": RT_PAIRS_HALVES, "neighbours": RT_PAIRS_NEIGHBOURS}[pairs], self._freq)
         _require(rt_qk_rotate_backward_workspace_bytes(self.cfg, 1) > 0, "QkRotate: shape")
 
-    def _inputs(self, q, k, pos, g_q, g_k, where):
-        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], self._t, q.device
-        _require(q.is_cuda and (k is not None or self.n_kv_heads == 0), where + ": q, k")
-        qp, qs = _rows(q, self.n_heads, hd, n, t, dev, where + ": q")
-        kp, ks = _rows(k, self.n_kv_heads, hd, n, t, dev, where + ": k") if self.n_kv_heads else (None, 0)
-        return (n, t, dev, qp, qs, kp, ks, _vector(g_q, self.n_heads * hd, t, dev, where + ": g_q"),
-                _vector(g_k, self.n_kv_heads * hd, t, dev, where + ": g_k"), _vector(pos, n, torch.int32, dev, where + ": pos"))
+    def _inputs(self, q, k, pos, g_q, g_k):
+        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], self._t, q.get_device()
+        _require(q.is_cuda and (k is not None or self.n_kv_heads == 0), "QkRotate: q, k")
+        qp, qs = _rows(q, self.n_heads, hd, n, t, dev, "QkRotate: q")
+        kp, ks = _rows(k, self.n_kv_heads, hd, n, t, dev, "QkRotate: k") if self.n_kv_heads else (None, 0)
+        return (n, t, dev, qp, qs, kp, ks, _vector(g_q, self.n_heads * hd, t, dev, "QkRotate: g_q"),
+                _vector(g_k, self.n_kv_heads * hd, t, dev, "QkRotate: g_k"), _vector(pos, n, torch.int32, dev, "QkRotate: pos"))
 
     def forward(self, q, k, pos, g_q=None, g_k=None, q_out=None, k_out=None):
         """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
         and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
         torch = _torch()
-        if q.is_cuda and torch.cuda.current_device() != q.device.index:
-            with torch.cuda.device(q.device):
+        if q.is_cuda and torch.cuda.current_device() != q.get_device():
+            with torch.cuda.device(q.get_device()):
                 return self.forward(q, k, pos, g_q, g_k, q_out, k_out)
-        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, "QkRotate.forward")
+        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
         qo, qos = _rows(q_out, self.n_heads, self.head_dim, n, t, dev, "QkRotate.forward: q_out")
         ko, kos = None, 0
         if self.n_kv_heads:
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
             ko, kos = _rows(k_out, self.n_kv_heads, self.head_dim, n, t, dev, "QkRotate.forward: k_out")
-        _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, _raw_stream(dev.index)), "rt_qk_rotate")
+        _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, _raw_stream(dev)), "rt_qk_rotate")
         return q_out, k_out
 
     def backward(self, q, k, pos, dq_out, dk_out, g_q=None, g_k=None, dq=None, dk=None):
         """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
         gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
         torch = _torch()
-        if q.is_cuda and torch.cuda.current_device() != q.device.index:
-            with torch.cuda.device(q.device):
+        if q.is_cuda and torch.cuda.current_device() != q.get_device():
+            with torch.cuda.device(q.get_device()):
                 return self.backward(q, k, pos, dq_out, dk_out, g_q, g_k, dq, dk)
-        where, f32, hd = "QkRotate.backward", torch.float32, self.head_dim
-        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k, where)
+        f32, hd = torch.float32, self.head_dim
+        n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
         kn = n * self.n_kv_heads * hd
         dq = torch.empty_like(dq_out) if dq is None else dq
         dk = (torch.empty_like(dk_out) if dk is None else dk) if self.n_kv_heads else None
         dgq = None if g_q is None else torch.empty_like(g_q, dtype=f32)
         dgk = None if g_k is None or not self.n_kv_heads else torch.empty_like(g_k, dtype=f32)
         ptr = lambda x: None if x is None else x.data_ptr()
-        ws = torch.empty(rt_qk_rotate_backward_workspace_bytes(self.cfg, n), dtype=torch.uint8, device=dev)
-        _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, where + ": dq_out"),
-                                     _vector(dk_out, kn, f32, dev, where + ": dk_out") if kn else None,
-                                     _vector(dq, n * self.n_heads * hd, f32, dev, where + ": dq"),
-                                     _vector(dk, kn, f32, dev, where + ": dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
-                                     _raw_stream(dev.index)), "rt_qk_rotate_backward")
+        ws = torch.empty(rt_qk_rotate_backward_workspace_bytes(self.cfg, n), dtype=torch.uint8, device=q.device)
+        _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, "QkRotate.backward: dq_out"),
+                                     _vector(dk_out, kn, f32, dev, "QkRotate.backward: dk_out") if kn else None,
+                                     _vector(dq, n * self.n_heads * hd, f32, dev, "QkRotate.backward: dq"),
+                                     _vector(dk, kn, f32, dev, "QkRotate.backward: dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
+                                     _raw_stream(dev)), "rt_qk_rotate_backward")
         return dq, dk, dgq, dgk
