@@ -26,46 +26,91 @@ __device__ __forceinline__ Lane lane_of(const RotateParams& p, int c) {
   return {4 * c, 4 * c + p.rot / 2};
 }
 
-__device__ __forceinline__ void load4(const float* p, float (&f)[4]) {
-  const float4 a = *reinterpret_cast<const float4*>(p);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&f)[4]) {
-  const uint2 a = *reinterpret_cast<const uint2*>(p);
-  f[0] = __uint_as_float(a.x << 16); f[1] = __uint_as_float(a.x & 0xffff0000u);
-  f[2] = __uint_as_float(a.y << 16); f[3] = __uint_as_float(a.y & 0xffff0000u);
-}
+// two fp32 numbers in a register pair: sm_100a multiplies and adds them in one instruction
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// a run of four elements as it lies in memory
+template <typename T> struct Run;
+template <> struct Run<float> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+};
+template <> struct Run<__nv_bfloat16> {
+  uint2 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float (&f)[4]) const {
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+};
 __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = make_uint2(pack2(a, b), pack2(c, d)); }
 
-// the eight elements of a lane as sides of pairs: x[i] = a, x[4 + i] = b
-template <typename T, bool NEIGHBOURS>
-__device__ __forceinline__ void load_pairs(const T* row, const Lane& l, float (&x)[8]) {
+// the two runs of a lane, and its pairs' sides: a[0] = sides a of pairs 0 and 1, a[1] of 2 and 3, b likewise
+template <typename T> struct Runs {
+  Run<T> x, y;
+  __device__ __forceinline__ void load(const T* row, const Lane& l) { x.load(row + l.first); y.load(row + l.second); }
+};
+struct Pairs { F2 a[2], b[2]; };
+template <bool NEIGHBOURS, typename T>
+__device__ __forceinline__ Pairs sides(const Runs<T>& r) {
   float u[4], v[4];
-  load4(row + l.first, u);
-  load4(row + l.second, v);
+  r.x.get(u);
+  r.y.get(v);
+  if (NEIGHBOURS) return {{f2(u[0], u[2]), f2(v[0], v[2])}, {f2(u[1], u[3]), f2(v[1], v[3])}};
+  return {{f2(u[0], u[1]), f2(u[2], u[3])}, {f2(v[0], v[1]), f2(v[2], v[3])}};
+}
+template <bool NEIGHBOURS, typename T>
+__device__ __forceinline__ void store_sides(T* row, const Lane& l, const Pairs& x) {
+  float a[4], b[4];
+  split(x.a[0], a[0], a[1]); split(x.a[1], a[2], a[3]); split(x.b[0], b[0], b[1]); split(x.b[1], b[2], b[3]);
   if (NEIGHBOURS) {
-    x[0] = u[0]; x[4] = u[1]; x[1] = u[2]; x[5] = u[3]; x[2] = v[0]; x[6] = v[1]; x[3] = v[2]; x[7] = v[3];
+    store4(row + l.first, a[0], b[0], a[1], b[1]);
+    store4(row + l.second, a[2], b[2], a[3], b[3]);
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = u[i]; x[4 + i] = v[i]; }
+    store4(row + l.first, a[0], a[1], a[2], a[3]);
+    store4(row + l.second, b[0], b[1], b[2], b[3]);
   }
 }
-template <typename T, bool NEIGHBOURS>
-__device__ __forceinline__ void store_pairs(T* row, const Lane& l, const float (&x)[8]) {
-  if (NEIGHBOURS) {
-    store4(row + l.first, x[0], x[4], x[1], x[5]);
-    store4(row + l.second, x[2], x[6], x[3], x[7]);
-  } else {
-    store4(row + l.first, x[0], x[1], x[2], x[3]);
-    store4(row + l.second, x[4], x[5], x[6], x[7]);
-  }
+__device__ __forceinline__ float dot(const Pairs& x, const Pairs& y) {        // of this lane's eight elements
+  F2 s = mul(x.a[0], y.a[0]);
+  s = fma(x.a[1], y.a[1], s);
+  s = fma(x.b[0], y.b[0], s);
+  s = fma(x.b[1], y.b[1], s);
+  float a, b;
+  split(s, a, b);
+  return a + b;
+}
+__device__ __forceinline__ Pairs times(const Pairs& x, const Pairs& y) { return {{mul(x.a[0], y.a[0]), mul(x.a[1], y.a[1])}, {mul(x.b[0], y.b[0]), mul(x.b[1], y.b[1])}}; }
+__device__ __forceinline__ Pairs times(const Pairs& x, float y) {
+  const F2 f = f2(y, y);
+  return {{mul(x.a[0], f), mul(x.a[1], f)}, {mul(x.b[0], f), mul(x.b[1], f)}};
+}
+__device__ __forceinline__ void add_to(Pairs& s, const Pairs& x, const Pairs& y) {       // s += x y
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { s.a[i] = fma(x.a[i], y.a[i], s.a[i]); s.b[i] = fma(x.b[i], y.b[i], s.b[i]); }
 }
 
-// cos and sin of this lane's four pairs.  Pair n's angle is formed by lane n % 32 of the warp; the turns are reduced in 64 bits, so that far
+// A row's angles as a lane needs them: cos and sin of its pairs 0, 1 and 2, 3.
+struct Turn {
+  F2 c[2], s[2], ns[2];
+  __device__ __forceinline__ Pairs forward(const Pairs& x) const {
+    return {{fma(x.a[0], c[0], mul(x.b[0], ns[0])), fma(x.a[1], c[1], mul(x.b[1], ns[1]))}, {fma(x.a[0], s[0], mul(x.b[0], c[0])), fma(x.a[1], s[1], mul(x.b[1], c[1]))}};
+  }
+  __device__ __forceinline__ Pairs back(const Pairs& x) const {
+    return {{fma(x.a[0], c[0], mul(x.b[0], s[0])), fma(x.a[1], c[1], mul(x.b[1], s[1]))}, {fma(x.a[0], ns[0], mul(x.b[0], c[0])), fma(x.a[1], ns[1], mul(x.b[1], c[1]))}};
+  }
+};
+
+// Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair; the turns are reduced in 64 bits, so that far
 // positions keep their angles.  All lanes of the warp call.
 template <int LPR>
-__device__ __forceinline__ void angles(const RotateParams& p, int pos, int lane, float (&cs)[4], float (&sn)[4]) {
+__device__ __forceinline__ Turn angles(const RotateParams& p, int pos, int lane) {
   constexpr int PER = LPR / 8;
   float co[PER], si[PER];
 #pragma unroll
@@ -78,6 +123,7 @@ __device__ __forceinline__ void angles(const RotateParams& p, int pos, int lane,
     }
   }
   const int c = lane % LPR;
+  float cs[4], sn[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int from = (4 * c + i) & 31;
@@ -88,62 +134,58 @@ __device__ __forceinline__ void angles(const RotateParams& p, int pos, int lane,
       if (4 * c + i >= 32) { cs[i] = c1; sn[i] = s1; }
     }
   }
-}
-__device__ __forceinline__ void turn(const float (&cs)[4], const float (&sn)[4], float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float a = x[i], b = x[4 + i];
-    x[i] = a * cs[i] - b * sn[i];
-    x[4 + i] = a * sn[i] + b * cs[i];
-  }
+  return {{f2(cs[0], cs[1]), f2(cs[2], cs[3])}, {f2(sn[0], sn[1]), f2(sn[2], sn[3])}, {f2(-sn[0], -sn[1]), f2(-sn[2], -sn[3])}};
 }
 
-// Block row y of the grid takes the heads [y * heads_per, ...) of every row: all of them where there are rows enough to fill the GPU, some of them in
-// small calls, where a warp's chain of heads would be the call's time.
-constexpr int kAhead = 4;       // loads in flight
+// The heads of a launch in block rows of the grid: heads_per of the queries' heads each, then heads_per of the keys' (a block row is either).  All of them
+// in one where there are rows enough to fill the GPU, some of them in small calls, where a warp's chain of heads would be the call's time.
+struct Part { bool is_q; int first, last; };
+__device__ __forceinline__ Part part_of(const RotateParams& p, int y, int heads_per) {
+  const int yq = (p.n_heads + heads_per - 1) / heads_per;
+  const bool is_q = y < yq;
+  const int first = (is_q ? y : y - yq) * heads_per;
+  return {is_q, first, min(is_q ? p.n_heads : p.n_kv, first + heads_per)};
+}
+
+constexpr int kAhead = 4;       // heads of a lane in flight
 template <typename T, int LPR, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per) {
+__global__ void __launch_bounds__(kThreads, 4) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per) {
   constexpr int HPW = 32 / LPR, HD = LPR * 8;
   const int lane = threadIdx.x & 31, hl = lane / LPR;
   const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
-  const int heads = p.n_heads + p.n_kv, first = blockIdx.y * heads_per, last = min(heads, first + heads_per);
+  const Part part = part_of(p, blockIdx.y, heads_per);
+  const T* in = (const T*)(part.is_q ? p.q : p.k);
+  T* out = (T*)(part.is_q ? p.q_out : p.k_out);
+  const T* g = p.norm ? (const T*)(part.is_q ? p.g_q : p.g_k) : nullptr;
+  const long long stride = part.is_q ? p.q_stride : p.k_stride, out_stride = part.is_q ? p.qo_stride : p.ko_stride;
   const long long warps = (long long)gridDim.x * (kThreads / 32);
   for (long long row = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); row < p.rows; row += warps) {
     const int pos = __ldg(p.pos + row);
-    if (pos < 0) continue;
-    float cs[4], sn[4];
-    const T *qr = (const T*)p.q + (size_t)row * p.q_stride, *kr = (const T*)p.k + (size_t)row * p.k_stride;
-    T *qo = (T*)p.q_out + (size_t)row * p.qo_stride, *ko = (T*)p.k_out + (size_t)row * p.ko_stride;
-    for (int h0 = first; h0 < last; h0 += HPW * kAhead) {
-      float x[kAhead][8];
+    Turn turn;
+    for (int h0 = part.first; h0 < part.last; h0 += HPW * kAhead) {
+      Runs<T> x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)                                 // (lanes without a head repeat the last one's for the shuffles)
+        x[u].load(in + (size_t)row * stride + min(h0 + u * HPW + hl, part.last - 1) * HD, l);
+      if (h0 == part.first) turn = angles<LPR>(p, pos, lane);
+      if (pos < 0) break;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int h = min(h0 + u * HPW + hl, last - 1);            // (lanes without a head repeat the last one's for the shuffles)
-        load_pairs<T, NEIGHBOURS>(h < p.n_heads ? qr + (size_t)h * HD : kr + (size_t)(h - p.n_heads) * HD, l, x[u]);
-      }
-      if (h0 == first) angles<LPR>(p, pos, lane, cs, sn);
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (h0 + u * HPW >= last) break;
-        const int hh = h0 + u * HPW + hl, h = min(hh, last - 1), hk = h - p.n_heads;
+        if (h0 + u * HPW >= part.last) break;
+        const int hh = h0 + u * HPW + hl, h = min(hh, part.last - 1);
+        Pairs y = sides<NEIGHBOURS>(x[u]);
         if (p.norm) {
-          float ss = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss += x[u][e] * x[u][e];
-          const float r = rsqrtf(row_sum<LPR>(ss) * (1.0f / HD) + p.eps);
-          const T* g = (const T*)(hk < 0 ? p.g_q : p.g_k);
+          const float r = rsqrtf(row_sum<LPR>(dot(y, y)) * (1.0f / HD) + p.eps);
           if (g) {
-            float gv[8];
-            load_pairs<T, NEIGHBOURS>(g + (size_t)(hk < 0 ? h : hk) * HD, l, gv);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[u][e] *= r * gv[e];
+            Runs<T> gr;
+            gr.load(g + h * HD, l);
+            y = times(y, times(sides<NEIGHBOURS>(gr), r));
           } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[u][e] *= r;
+            y = times(y, r);
           }
         }
-        turn(cs, sn, x[u]);
-        if (hh < last) store_pairs<T, NEIGHBOURS>(hk < 0 ? qo + (size_t)h * HD : ko + (size_t)hk * HD, l, x[u]);
+        y = turn.forward(y);
+        if (hh < part.last) store_sides<NEIGHBOURS>(out + (size_t)row * out_stride + h * HD, l, y);
       }
     }
   }
@@ -152,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant_
 // Backward: block (x, y) takes rows [x * chunk, (x + 1) * chunk) of the HPW heads that lie side by side in a warp, its warps a row each.  The gains' partial
 // sums of its rows go to part[x][heads * HD], added up by sum_parts_kernel in the order of x.
 template <typename T, int LPR, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
+__global__ void __launch_bounds__(kThreads, 3) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
   constexpr int HPW = 32 / LPR, HD = LPR * 8, ROWS = kThreads / 32, AHEAD = 2;
   __shared__ float red[ROWS][HPW * HD];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPR, hl = lane / LPR;
@@ -167,51 +209,47 @@ __global__ void __launch_bounds__(kThreads) rotate_backward_kernel(const __grid_
   const float* d0 = (is_q ? p.dq_out : p.dk_out) + (size_t)h * HD;
   float* o0 = (is_q ? p.dq : p.dk) + (size_t)h * HD;
   const T* g = p.norm ? (const T*)(is_q ? p.g_q : p.g_k) : nullptr;
-  float gv[8], dg[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) { gv[e] = 1.0f; dg[e] = 0.0f; }
-  if (g) load_pairs<T, NEIGHBOURS>(g + (size_t)h * HD, l, gv);
+  const F2 zero = f2(0.f, 0.f), one = f2(1.f, 1.f);
+  Pairs gv = {{one, one}, {one, one}}, dg = {{zero, zero}, {zero, zero}};
+  if (g) {
+    Runs<T> gr;
+    gr.load(g + (size_t)h * HD, l);
+    gv = sides<NEIGHBOURS>(gr);
+  }
   const long long r0 = (long long)blockIdx.x * chunk, r1 = min((long long)p.rows, r0 + chunk);
   for (long long rb = r0 + warp; rb < r1; rb += ROWS * AHEAD) {
-    float x[AHEAD][8], d[AHEAD][8];
+    Runs<T> x[AHEAD];
+    Runs<float> d[AHEAD];
     int pos[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const long long row = min(rb + u * ROWS, r1 - 1);
       pos[u] = __ldg(p.pos + row);
-      load_pairs<T, NEIGHBOURS>(x0 + (size_t)row * stride, l, x[u]);
-      load_pairs<float, NEIGHBOURS>(d0 + (size_t)row * gstride, l, d[u]);
+      x[u].load(x0 + (size_t)row * stride, l);
+      d[u].load(d0 + (size_t)row * gstride, l);
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const long long row = rb + u * ROWS;
       if (row >= r1 || pos[u] < 0) continue;
-      float cs[4], sn[4];
-      angles<LPR>(p, pos[u], lane, cs, sn);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sn[i] = -sn[i];
-      turn(cs, sn, d[u]);
+      const Turn turn = angles<LPR>(p, pos[u], lane);
+      Pairs w = turn.back(sides<NEIGHBOURS>(d[u]));
       if (p.norm) {
-        float ss = 0.f, du = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss += x[u][e] * x[u][e];
-        const float r = rsqrtf(row_sum<LPR>(ss) * (1.0f / HD) + p.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[u][e] *= r;
-          dg[e] += d[u][e] * x[u][e];
-          d[u][e] *= gv[e];
-          du += d[u][e] * x[u][e];
-        }
-        const float mean = row_sum<LPR>(du) * (1.0f / HD);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[u][e] = r * (d[u][e] - x[u][e] * mean);
+        Pairs y = sides<NEIGHBOURS>(x[u]);
+        const float r = rsqrtf(row_sum<LPR>(dot(y, y)) * (1.0f / HD) + p.eps);
+        y = times(y, r);
+        add_to(dg, w, y);
+        w = times(w, gv);
+        const float mean = row_sum<LPR>(dot(w, y)) * (1.0f / HD);
+        const Pairs m = {{f2(-mean, -mean), f2(-mean, -mean)}, {f2(-mean, -mean), f2(-mean, -mean)}};
+        add_to(w, y, m);
+        w = times(w, r);
       }
-      if (head_in) store_pairs<float, NEIGHBOURS>(o0 + (size_t)row * gstride, l, d[u]);
+      if (head_in) store_sides<NEIGHBOURS>(o0 + (size_t)row * gstride, l, w);
     }
   }
   if (!part) return;
-  store_pairs<float, NEIGHBOURS>(&red[warp][hl * HD], l, dg);
+  store_sides<NEIGHBOURS>(&red[warp][hl * HD], l, dg);
   __syncthreads();
   for (int i = threadIdx.x; i < HPW * HD; i += kThreads) {
     if (blockIdx.y * HPW + i / HD >= heads) continue;
@@ -251,11 +289,11 @@ template <typename T, int LPR>
 cudaError_t forward(const RotateParams& p, cudaStream_t s) {
   constexpr int HPW = 32 / LPR;
   const long long blocks = ((long long)p.rows + kThreads / 32 - 1) / (kThreads / 32);
-  const int heads = p.n_heads + p.n_kv;
+  const int most = max(p.n_heads, p.n_kv);
   // at least two blocks for each SM if the heads allow it
-  const int ways = (int)min((long long)ceil_div(heads, HPW), max(1LL, 148 * 2 / blocks));
-  const int heads_per = ways == 1 ? heads : max(HPW, ceil_div(ceil_div(heads, ways), HPW) * HPW);
-  const dim3 grid((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64), ceil_div(heads, heads_per));
+  const int ways = (int)min((long long)ceil_div(most, HPW), max(1LL, 148 * 2 / blocks));
+  const int heads_per = ceil_div(ceil_div(most, ways), HPW) * HPW;
+  const dim3 grid((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64), ceil_div(p.n_heads, heads_per) + ceil_div(p.n_kv, heads_per));
   if (p.neighbours) rotate_kernel<T, LPR, true><<<grid, kThreads, 0, s>>>(p, heads_per);
   else rotate_kernel<T, LPR, false><<<grid, kThreads, 0, s>>>(p, heads_per);
   return cudaGetLastError();

@@ -646,8 +646,8 @@ class PagedCache:
                 return self.read(seq, pos, dtype, k, v)
         t = _tdtype(dtype)
         shape = (n, c.n_kv_heads, c.head_dim)
-        k = torch.empty(shape, dtype=t, device=self.device) if k is None else k
-        v = torch.empty(shape, dtype=t, device=self.device) if v is None else v
+        k = self.k.new_empty(shape, dtype=t) if k is None else k
+        v = self.k.new_empty(shape, dtype=t) if v is None else v
         kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: k")
         vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: v")
         sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.read: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.read: pos")
