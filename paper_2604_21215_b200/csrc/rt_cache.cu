@@ -109,10 +109,11 @@ template <int LPR> struct Held<__nv_fp8_e4m3, LPR> {
 };
 
 // A warp takes the keys or the values of rows_per consecutive rows (at most 32).  Its lanes look their places up together, one row each: the chain row ->
-// page table -> place costs two trips to memory however many rows there are.
+// page table -> place costs two trips to memory however many rows there are.  Then it goes through the rows' heads, the next loads always under way.
 template <typename T, typename CT, int LPR, bool WRITE>
-__global__ void __launch_bounds__(kThreads) cache_rows_kernel(const __grid_constant__ CacheRowsParams p, int rows_per) {
-  constexpr int HPW = 32 / LPR, HD = LPR * 16, AHEAD = 2;          // heads side by side in a warp; passes in flight
+__global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_constant__ CacheRowsParams p, int rows_per) {
+  constexpr int HPW = 32 / LPR, HD = LPR * 16;                     // heads side by side in a warp
+  constexpr int AHEAD = sizeof(T) == 4 && WRITE ? 1 : 2;           // passes over the heads in flight, and as many on their way
   const int lane = threadIdx.x & 31, c = lane % LPR, hl = lane / LPR, n_kv = p.c.n_kv_heads;
   const long long w = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), r0 = (w >> 1) * rows_per;
   const bool is_v = w & 1;
@@ -133,52 +134,60 @@ __global__ void __launch_bounds__(kThreads) cache_rows_kernel(const __grid_const
       if (page >= 0) place = (long long)page * n_kv * p.c.page_size + (t & (p.c.page_size - 1));
     }
   }
-  for (int i = 0; i < n; ++i) {
-    const long long row0 = __shfl_sync(0xffffffffu, place, i);
-    if (row0 < 0) continue;
-    for (int h0 = hl; h0 - hl < n_kv; h0 += HPW * AHEAD) {
+  struct Buffer { Run<T> x[WRITE ? AHEAD : 1][2]; Held<CT, LPR> y[WRITE ? 1 : AHEAD]; };
+  // (lanes without a head repeat the last one's for the shuffles; rows that are not in use are read from place 0, which is there, and left)
+  auto load = [&](Buffer& b, int i, int h0) {
+    const size_t row0 = (size_t)max(__shfl_sync(0xffffffffu, place, i), 0LL);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int h = min(h0 + u * HPW + hl, n_kv - 1);
       if constexpr (WRITE) {
-        Run<T> x[AHEAD][2];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const int h = min(h0 + u * HPW, n_kv - 1);               // (lanes without a head repeat the last one's for the shuffles)
-          const T* from = in + (size_t)i * stride + h * HD;
-          x[u][0].load(from + c * 8);
-          x[u][1].load(from + (c + LPR) * 8);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const int h = h0 + u * HPW;
-          const size_t row = (size_t)row0 + (size_t)min(h, n_kv - 1) * p.c.page_size;
-          put_row<T, CT, LPR>(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c, h < n_kv, x[u]);
-        }
+        const T* from = in + (size_t)i * stride + h * HD;
+        b.x[u][0].load(from + c * 8);
+        b.x[u][1].load(from + (c + LPR) * 8);
       } else {
-        Held<CT, LPR> x[AHEAD];
+        const size_t row = row0 + (size_t)h * p.c.page_size;
+        b.y[u].load(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c);
+      }
+    }
+  };
+  Buffer now, next;
+  int i = 0, h0 = 0;
+  load(now, 0, 0);
+  while (true) {
+    const bool row_ends = h0 + HPW * AHEAD >= n_kv;
+    const int ni = row_ends ? i + 1 : i, nh = row_ends ? 0 : h0 + HPW * AHEAD;
+    if (ni < n) load(next, ni, nh);
+    const long long row0 = __shfl_sync(0xffffffffu, place, i);
+    if (row0 >= 0) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const size_t row = (size_t)row0 + (size_t)min(h0 + u * HPW, n_kv - 1) * p.c.page_size;
-          x[u].load(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const int h = h0 + u * HPW;
-          if (h >= n_kv) continue;
+      for (int u = 0; u < AHEAD; ++u) {
+        const int h = h0 + u * HPW + hl;
+        if (h - hl >= n_kv) break;
+        if constexpr (WRITE) {
+          const size_t row = (size_t)row0 + (size_t)min(h, n_kv - 1) * p.c.page_size;
+          put_row<T, CT, LPR>(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c, h < n_kv, now.x[u]);
+        } else if (h < n_kv) {
           T* to = out + (size_t)i * stride + h * HD;
           float f[8];
-          x[u].get(0, f);
+          now.y[u].get(0, f);
           store8(to + c * 8, f);
-          x[u].get(1, f);
+          now.y[u].get(1, f);
           store8(to + (c + LPR) * 8, f);
         }
       }
     }
+    if (ni >= n) break;
+    i = ni;
+    h0 = nh;
+    now = next;
   }
 }
 
 template <typename T, typename CT, bool WRITE>
 cudaError_t launch(const CacheRowsParams& p, cudaStream_t s) {
-  // several rows a warp once there are rows for 48 warps on every SM
-  const int rows_per = (int)min(8LL, max(1LL, (long long)p.rows * 2 / (148 * 48)));
+  // several rows a warp once there are more than the GPU's warps (24 an SM) take one of
+  const int rows_per = (int)min(32LL, max(1LL, ((long long)p.rows * 2 + 148 * 24 - 1) / (148 * 24)));
   const long long warps = ((long long)p.rows + rows_per - 1) / rows_per * 2;
   const dim3 grid((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32)));
   if (p.c.head_dim == 64) cache_rows_kernel<T, CT, 4, WRITE><<<grid, kThreads, 0, s>>>(p, rows_per);

@@ -147,55 +147,90 @@ __device__ __forceinline__ Part part_of(const RotateParams& p, int y, int heads_
   return {is_q, first, min(is_q ? p.n_heads : p.n_kv, first + heads_per)};
 }
 
-constexpr int kAhead = 4;       // heads of a lane in flight
-template <typename T, int LPR, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads, 4) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per) {
-  constexpr int HPW = 32 / LPR, HD = LPR * 8;
+constexpr int kBlocks = 3;      // of an SM, by registers
+template <typename T> constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;       // heads of a lane in flight, and as many on their way
+// WHOLE: every block row's heads fill whole batches of kAhead (otherwise lanes without a head repeat the last one's, for the shuffles).
+template <typename T, int LPR, bool NEIGHBOURS, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per) {
+  constexpr int HPW = 32 / LPR, HD = LPR * 8, AHEAD = kAhead<T>, BATCH = HPW * AHEAD;
   const int lane = threadIdx.x & 31, hl = lane / LPR;
   const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
   const Part part = part_of(p, blockIdx.y, heads_per);
+  const int first = part.first, last = part.last;
   const T* in = (const T*)(part.is_q ? p.q : p.k);
   T* out = (T*)(part.is_q ? p.q_out : p.k_out);
   const T* g = p.norm ? (const T*)(part.is_q ? p.g_q : p.g_k) : nullptr;
-  const long long stride = part.is_q ? p.q_stride : p.k_stride, out_stride = part.is_q ? p.qo_stride : p.ko_stride;
-  const long long warps = (long long)gridDim.x * (kThreads / 32);
-  for (long long row = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); row < p.rows; row += warps) {
-    const int pos = __ldg(p.pos + row);
-    Turn turn;
-    for (int h0 = part.first; h0 < part.last; h0 += HPW * kAhead) {
-      Runs<T> x[kAhead];
+  const size_t stride = part.is_q ? p.q_stride : p.k_stride, out_stride = part.is_q ? p.qo_stride : p.ko_stride;
+  const unsigned warps = gridDim.x * (kThreads / 32), rows = p.rows;
+  unsigned row = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  // the u-th head of a batch that begins at h0, from the row's start (its elements are read and written once each, so q_out may be q)
+  auto at = [&](int h0, int u) { return WHOLE ? (h0 + hl) * HD + u * HPW * HD : min(h0 + hl + u * HPW, last - 1) * HD; };
+  Runs<T> x[AHEAD], next[AHEAD];
+  auto load = [&](Runs<T> (&to)[AHEAD], unsigned r, int h0) {
+    const T* from = in + r * stride;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)                                 // (lanes without a head repeat the last one's for the shuffles)
-        x[u].load(in + (size_t)row * stride + min(h0 + u * HPW + hl, part.last - 1) * HD, l);
-      if (h0 == part.first) turn = angles<LPR>(p, pos, lane);
-      if (pos < 0) break;
+    for (int u = 0; u < AHEAD; ++u) to[u].load(from + at(h0, u), l);
+  };
+  int pos = __ldg(p.pos + row), next_pos = 0, h0 = first;
+  load(x, row, h0);
+  Turn turn = angles<LPR>(p, pos, lane);
+  while (true) {
+    const bool row_ends = h0 + BATCH >= last;
+    const unsigned nr = row_ends ? row + warps : row;
+    const int nh = row_ends ? first : h0 + BATCH;
+    const bool more = nr < rows && nr >= row;
+    if (more) {
+      if (row_ends) next_pos = __ldg(p.pos + nr);
+      load(next, nr, nh);
+    }
+    if (pos >= 0) {
+      T* to = out + row * out_stride;
+      Runs<T> gr[AHEAD];
+      float r[AHEAD];
+      if (p.norm) {
+        // the gains on their way, and the heads' sums side by side: a sum alone would wait for each of its shuffles
+        if (g) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (h0 + u * HPW >= part.last) break;
-        const int hh = h0 + u * HPW + hl, h = min(hh, part.last - 1);
-        Pairs y = sides<NEIGHBOURS>(x[u]);
-        if (p.norm) {
-          const float r = rsqrtf(row_sum<LPR>(dot(y, y)) * (1.0f / HD) + p.eps);
-          if (g) {
-            Runs<T> gr;
-            gr.load(g + h * HD, l);
-            y = times(y, times(sides<NEIGHBOURS>(gr), r));
-          } else {
-            y = times(y, r);
-          }
+          for (int u = 0; u < AHEAD; ++u) gr[u].load(g + at(h0, u), l);
         }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          const Pairs y = sides<NEIGHBOURS>(x[u]);
+          r[u] = dot(y, y);
+        }
+#pragma unroll
+        for (int o = LPR / 2; o; o >>= 1)
+#pragma unroll
+          for (int u = 0; u < AHEAD; ++u) r[u] += __shfl_xor_sync(0xffffffffu, r[u], o);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) r[u] = rsqrtf(r[u] * (1.0f / HD) + p.eps);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        Pairs y = sides<NEIGHBOURS>(x[u]);
+        if (p.norm) y = g ? times(y, times(sides<NEIGHBOURS>(gr[u]), r[u])) : times(y, r[u]);
         y = turn.forward(y);
-        if (hh < part.last) store_sides<NEIGHBOURS>(out + (size_t)row * out_stride + h * HD, l, y);
+        if (WHOLE || h0 + hl + u * HPW < last) store_sides<NEIGHBOURS>(to + at(h0, u), l, y);
       }
     }
+    if (!more) break;
+    if (row_ends) {
+      pos = next_pos;
+      turn = angles<LPR>(p, pos, lane);
+    }
+    row = nr;
+    h0 = nh;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) x[u] = next[u];
   }
 }
 
 // Backward: block (x, y) takes rows [x * chunk, (x + 1) * chunk) of the HPW heads that lie side by side in a warp, its warps a row each.  The gains' partial
 // sums of its rows go to part[x][heads * HD], added up by sum_parts_kernel in the order of x.
 template <typename T, int LPR, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads, 3) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
-  constexpr int HPW = 32 / LPR, HD = LPR * 8, ROWS = kThreads / 32, AHEAD = 2;
+__global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
+  constexpr int HPW = 32 / LPR, HD = LPR * 8, ROWS = kThreads / 32, AHEAD = 1;
   __shared__ float red[ROWS][HPW * HD];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPR, hl = lane / LPR;
   const Lane l = lane_of<NEIGHBOURS>(p, c);
@@ -293,9 +328,13 @@ cudaError_t forward(const RotateParams& p, cudaStream_t s) {
   // at least two blocks for each SM if the heads allow it
   const int ways = (int)min((long long)ceil_div(most, HPW), max(1LL, 148 * 2 / blocks));
   const int heads_per = ceil_div(ceil_div(most, ways), HPW) * HPW;
-  const dim3 grid((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64), ceil_div(p.n_heads, heads_per) + ceil_div(p.n_kv, heads_per));
-  if (p.neighbours) rotate_kernel<T, LPR, true><<<grid, kThreads, 0, s>>>(p, heads_per);
-  else rotate_kernel<T, LPR, false><<<grid, kThreads, 0, s>>>(p, heads_per);
+  const int parts = ceil_div(p.n_heads, heads_per) + ceil_div(p.n_kv, heads_per);
+  const long long most_blocks = max(1, 148 * kBlocks / parts);               // what the GPU holds at once: a warp goes on to its next row with that row's loads under way
+  const dim3 grid((unsigned)min(blocks, most_blocks), parts);
+  const bool whole = heads_per % (HPW * kAhead<T>) == 0 && p.n_heads % heads_per == 0 && p.n_kv % heads_per == 0;
+  auto* kernel = p.neighbours ? (whole ? rotate_kernel<T, LPR, true, true> : rotate_kernel<T, LPR, true, false>)
+                              : (whole ? rotate_kernel<T, LPR, false, true> : rotate_kernel<T, LPR, false, false>);
+  kernel<<<grid, kThreads, 0, s>>>(p, heads_per);
   return cudaGetLastError();
 }
 
