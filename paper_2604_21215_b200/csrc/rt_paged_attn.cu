@@ -884,7 +884,7 @@ cudaError_t launch_split(const PagedAttnParams& p, float* part, cudaStream_t s) 
   const cudaError_t e1 = cudaGetLastError();
   if (e1 != cudaSuccess || most <= (long long)p.c.n_seqs * p.c.n_kv_heads * slices) return e1;
   const long long heads = (long long)p.c.n_seqs * p.q.n_heads;
-  return launch_chained(paged_join_kernel<S::KT, HD>, dim3((unsigned)(heads < kSms * 4 ? heads : kSms * 4)), dim3(kJoinWarps * 32), 0, s, true, p,
+  return launch_chained(paged_join_kernel<S::KT, HD>, dim3((unsigned)(heads < kSms * 6 ? heads : kSms * 6)), dim3(kJoinWarps * 32), 0, s, true, p,
                         (const float*)part, part_rows_of(p.group), S::WORKERS);
 }
 

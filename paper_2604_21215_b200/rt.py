@@ -328,21 +328,21 @@ def _raw_stream(index: int) -> int:
 
 def _rows(t, heads: int, head_dim: int, n: int, dtype, index: int, where: str) -> tuple:
     """(address, stride) of [n, heads, head_dim] or [n, heads * head_dim] rows on CUDA device `index` whose heads are contiguous."""
-    st, sh = t.stride(), t.shape
-    if len(sh) == 3:
-        ok = sh[1] == heads and sh[2] == head_dim and st[2] == 1 and (heads == 1 or st[1] == head_dim)
-    else:
-        ok = len(sh) == 2 and sh[1] == heads * head_dim and st[1] == 1
-    if not ok or sh[0] != n or t.dtype != dtype or t.get_device() != index:
-        raise RtError(RT_ERR_INVALID_ARG, where)
-    return t.data_ptr(), st[0]
+    if t.dtype is dtype and t.get_device() == index:
+        sh = t.shape
+        if t.is_contiguous() and (sh == (n, heads, head_dim) or sh == (n, heads * head_dim)):
+            return t.data_ptr(), heads * head_dim
+        st = t.stride()
+        if (sh == (n, heads, head_dim) and st[2] == 1 and (heads == 1 or st[1] == head_dim)) or (sh == (n, heads * head_dim) and st[1] == 1):
+            return t.data_ptr(), st[0]
+    raise RtError(RT_ERR_INVALID_ARG, where)
 
 
 def _vector(t, n: int, dtype, index: int, where: str):
     """Address of a contiguous array of n elements on CUDA device `index`, None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or t.get_device() != index or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != index or not t.is_contiguous():
         raise RtError(RT_ERR_INVALID_ARG, where)
     return t.data_ptr()
 
@@ -628,7 +628,7 @@ class PagedCache:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
         seq[r] (int32); a negative position skips the row."""
         torch, c, dev, n = _torch(), self._c, self._index, k.shape[0]
-        if torch.cuda.current_device() != dev:
+        if torch._C._cuda_getDevice() != dev:
             with torch.cuda.device(dev):
                 return self.write(k, v, seq, pos)
         _require(k.dtype in self._codes, "PagedCache.write: k")
@@ -641,7 +641,7 @@ class PagedCache:
         """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
         Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
         torch, c, dev, n = _torch(), self._c, self._index, pos.shape[0]
-        if torch.cuda.current_device() != dev:
+        if torch._C._cuda_getDevice() != dev:
             with torch.cuda.device(dev):
                 return self.read(seq, pos, dtype, k, v)
         t = _tdtype(dtype)
@@ -660,7 +660,7 @@ class PagedCache:
         [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
         whatever the memory holds)."""
         torch, c, dev = _torch(), self._c, self._index
-        if torch.cuda.current_device() != dev:
+        if torch._C._cuda_getDevice() != dev:
             with torch.cuda.device(dev):
                 return self.attend(q, lens, k_own, v_own, scale, alibi_slopes, out, lse)
         B, kv, hd = c.n_seqs, c.n_kv_heads, c.head_dim
@@ -722,7 +722,7 @@ class QkRotate:
         """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
         and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
         torch = _torch()
-        if q.is_cuda and torch.cuda.current_device() != q.get_device():
+        if q.is_cuda and torch._C._cuda_getDevice() != q.get_device():
             with torch.cuda.device(q.get_device()):
                 return self.forward(q, k, pos, g_q, g_k, q_out, k_out)
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
@@ -739,7 +739,7 @@ class QkRotate:
         """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
         gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
         torch = _torch()
-        if q.is_cuda and torch.cuda.current_device() != q.get_device():
+        if q.is_cuda and torch._C._cuda_getDevice() != q.get_device():
             with torch.cuda.device(q.get_device()):
                 return self.backward(q, k, pos, dq_out, dk_out, g_q, g_k, dq, dk)
         f32, hd = torch.float32, self.head_dim
