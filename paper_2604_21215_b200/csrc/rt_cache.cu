@@ -135,51 +135,45 @@ __global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_co
     }
   }
   struct Buffer { Run<T> x[WRITE ? AHEAD : 1][2]; Held<CT, LPR> y[WRITE ? 1 : AHEAD]; };
-  // (lanes without a head repeat the last one's for the shuffles; rows that are not in use are read from place 0, which is there, and left)
-  auto load = [&](Buffer& b, int i, int h0) {
-    const size_t row0 = (size_t)max(__shfl_sync(0xffffffffu, place, i), 0LL);
+  // The rows' heads in one line, HPW side by side: head y % n_kv of row y / n_kv.  (Lanes behind the end repeat the last one for the shuffles; rows that are
+  // not in use are read from place 0, which is there, and left.)
+  const int total = n * n_kv;
+  auto load = [&](Buffer& b, int y0) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int h = min(h0 + u * HPW + hl, n_kv - 1);
+      const int y = min(y0 + u * HPW + hl, total - 1), i = y / n_kv, h = y - i * n_kv;
       if constexpr (WRITE) {
         const T* from = in + (size_t)i * stride + h * HD;
         b.x[u][0].load(from + c * 8);
         b.x[u][1].load(from + (c + LPR) * 8);
       } else {
-        const size_t row = row0 + (size_t)h * p.c.page_size;
+        const size_t row = (size_t)max(__shfl_sync(0xffffffffu, place, i), 0LL) + (size_t)h * p.c.page_size;
         b.y[u].load(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c);
       }
     }
   };
   Buffer now, next;
-  int i = 0, h0 = 0;
-  load(now, 0, 0);
-  while (true) {
-    const bool row_ends = h0 + HPW * AHEAD >= n_kv;
-    const int ni = row_ends ? i + 1 : i, nh = row_ends ? 0 : h0 + HPW * AHEAD;
-    if (ni < n) load(next, ni, nh);
-    const long long row0 = __shfl_sync(0xffffffffu, place, i);
-    if (row0 >= 0) {
+  load(now, 0);
+  for (int y0 = 0; y0 < total; y0 += HPW * AHEAD) {
+    if (y0 + HPW * AHEAD < total) load(next, y0 + HPW * AHEAD);
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int h = h0 + u * HPW + hl;
-        if (h - hl >= n_kv) break;
-        if constexpr (WRITE) {
-          const size_t row = (size_t)row0 + (size_t)min(h, n_kv - 1) * p.c.page_size;
-          put_row<T, CT, LPR>(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c, h < n_kv, now.x[u]);
-        } else if (h < n_kv) {
-          T* to = out + (size_t)i * stride + h * HD;
-          float f[8];
-          now.y[u].get(0, f);
-          store8(to + c * 8, f);
-          now.y[u].get(1, f);
-          store8(to + (c + LPR) * 8, f);
-        }
+    for (int u = 0; u < AHEAD; ++u) {
+      if (y0 + u * HPW >= total) break;
+      const int y = y0 + u * HPW + hl, yc = min(y, total - 1), i = yc / n_kv, h = yc - i * n_kv;
+      const long long row0 = __shfl_sync(0xffffffffu, place, i);
+      const bool ok = y < total && row0 >= 0;
+      if constexpr (WRITE) {
+        const size_t row = (size_t)max(row0, 0LL) + (size_t)h * p.c.page_size;
+        put_row<T, CT, LPR>(pool + row * HD, exps + (sizeof(CT) == 1 ? row : 0), c, ok, now.x[u]);
+      } else if (ok) {
+        T* to = out + (size_t)i * stride + h * HD;
+        float f[8];
+        now.y[u].get(0, f);
+        store8(to + c * 8, f);
+        now.y[u].get(1, f);
+        store8(to + (c + LPR) * 8, f);
       }
     }
-    if (ni >= n) break;
-    i = ni;
-    h0 = nh;
     now = next;
   }
 }

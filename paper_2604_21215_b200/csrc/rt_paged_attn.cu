@@ -796,10 +796,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
   }
 }
 
-// Joins the heads that several warps of the kernel above share: a block takes a query head, its warps every kJoinWarps-th partial result.  It
+// Joins the heads that several warps of the kernel above share: a block takes a query head, its warps every kJoinWarps-th partial result
+// (maxima and sums first, one result a lane, then outputs with known weights: two trips to memory for up to 32 a warp).  It
 // starts beside that kernel (programmatic launch): all that does not depend on its results is done before the wait.
-constexpr int kJoinWarps = 8;
-template <int KT, int HD>
+template <int KT, int HD, int kJoinWarps>
 __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __grid_constant__ PagedAttnParams p, const float* part, int part_rows, int max_workers) {
   __shared__ unsigned sums[kJoinWarps * 32], warp_sums[kJoinWarps];
   __shared__ float sm_o[kJoinWarps][HD], sm_m[kJoinWarps], sm_l[kJoinWarps];
@@ -826,15 +826,27 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __gri
     float m = -INFINITY, l = 0.f, o[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
-#pragma unroll 2
-    for (unsigned w = w0 + warp; w <= w1; w += kJoinWarps) {
-      const float* slot = part + ((size_t)w * 2 + (w == w0 ? 1 : 0)) * slot_floats(part_rows, HD);
-      const float ms = slot[part_rows * HD + 2 * r], ls = slot[part_rows * HD + 2 * r + 1];
-      const float mn = fmaxf(m, ms), ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(m - ref), f1 = ex2(ms - ref);
+    auto slot = [&](unsigned w) { return part + ((size_t)w * 2 + (w == w0 ? 1 : 0)) * slot_floats(part_rows, HD); };
+    for (unsigned first = w0 + warp; first <= w1; first += 32 * kJoinWarps) {
+      const unsigned mine = first + lane * kJoinWarps;
+      float ms = -INFINITY, ls = 0.f;
+      if (mine <= w1) {
+        const float* s = slot(mine) + part_rows * HD + 2 * r;
+        ms = s[0]; ls = s[1];
+      }
+      const float mn = fmaxf(m, warp_max(ms)), ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(m - ref), f = ex2(ms - ref);
       m = mn;
-      l = l * f0 + ls * f1;
+      l = l * f0 + warp_sum(ls * f);
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) o[d] = o[d] * f0 + slot[r * HD + d * 32 + lane] * f1;
+      for (int d = 0; d < HD / 32; ++d) o[d] *= f0;
+      const int n = (int)min(32u, (w1 - first) / kJoinWarps + 1);
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float fk = __shfl_sync(0xffffffffu, f, k);
+        const float* s = slot(first + k * kJoinWarps) + r * HD + lane;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) o[d] += s[d * 32] * fk;
+      }
     }
     __syncthreads();                                                   // (the arrays of the head before are read)
 #pragma unroll
@@ -884,8 +896,10 @@ cudaError_t launch_split(const PagedAttnParams& p, float* part, cudaStream_t s) 
   const cudaError_t e1 = cudaGetLastError();
   if (e1 != cudaSuccess || most <= (long long)p.c.n_seqs * p.c.n_kv_heads * slices) return e1;
   const long long heads = (long long)p.c.n_seqs * p.q.n_heads;
-  return launch_chained(paged_join_kernel<S::KT, HD>, dim3((unsigned)(heads < kSms * 6 ? heads : kSms * 6)), dim3(kJoinWarps * 32), 0, s, true, p,
-                        (const float*)part, part_rows_of(p.group), S::WORKERS);
+  // eight warps a head; two where there are more heads than such blocks at once (200 x 12 heads: 25 us against 28)
+  const int rows = part_rows_of(p.group);
+  if (heads <= kSms * 6) return launch_chained(paged_join_kernel<S::KT, HD, 8>, dim3((unsigned)heads), dim3(256), 0, s, true, p, (const float*)part, rows, S::WORKERS);
+  return launch_chained(paged_join_kernel<S::KT, HD, 2>, dim3((unsigned)(heads < kSms * 24 ? heads : kSms * 24)), dim3(64), 0, s, true, p, (const float*)part, rows, S::WORKERS);
 }
 
 template <typename CT, int HD>
