@@ -918,7 +918,7 @@ cudaError_t launch_simt(const PagedAttnParams& p, float* part, cudaStream_t s) {
 
 bool paged_attn_counts(const rt_paged_cache* c, int n_heads) {
   const long long items = (long long)c->n_kv_heads * ceil_div(n_heads / c->n_kv_heads, kRows), units = (long long)c->max_pages * (c->page_size / 16);
-  return units <= 0x7fffffffLL / items / c->n_seqs && (long long)c->max_pages * c->page_size <= 0x7fffffffLL;
+  return units <= 0x7fffffffLL / items / c->n_seqs && (long long)c->max_pages * c->page_size <= 1LL << 30;
 }
 
 size_t paged_attn_workspace(const rt_paged_cache* c, int n_heads) {

@@ -578,3 +578,99 @@ def test_tensors_that_are_refused():
     for f in refused:
         with pytest.raises(rt.RtError):
             f()
+
+
+# ---------------------------------------------------------------- together
+
+@pytest.mark.parametrize("cache", ["f32", "e4m3"])
+def test_a_recurrent_layer_goes_on_from_pages_of_ragged_length(cache):
+    """A batch that one layer has prefilled together goes on from different lengths: its pairs move into pages, and each step norms (no rotation: rot_dim 0)
+    queries and keys, attends over the pages and the temporary pair, and writes the persistent pair of the layer's output."""
+    from oracle import RTConfig, RTWeights, layer_seq
+    from paper_2604_21215_b200 import inputs
+    rt = rt_module()
+    d, H, dff, B, N = 128, 2, 512, 4, 60
+    slopes = [0.25, 0.0625]
+    data = inputs.make_inputs(inputs.Workload("pages", 1, B, N, d, H, dff, "f32"), seed=5)
+    lw = dict(data["layers"][0], alibi_slopes=slopes)
+    rng = np.random.default_rng(6)
+    for n in ("g_attn", "g_mlp", "g_kv", "g_q", "g_k"):
+        lw[n] = (1 + 0.2 * rng.standard_normal(d)).astype(np.float32).astype(np.float64)
+    x = data["x"]
+    ocfg = RTConfig(d, H, 64, dff, alibi_slopes=slopes)
+    z_ref, _, _ = layer_seq(ocfg, RTWeights(**{n: v for n, v in lw.items() if n != "alibi_slopes"}), x)
+    layer = rt.Layer(d, H, dff, dtype="f32", leaf=16)
+    layer.set_weights(lw)
+    lens, steps = [0, 1, 37, 56], 4                                     # what each sequence keeps of the prefill, and how far it goes on
+    layer.prefill(x[:, :56], N_max=56)
+    c = rt.PagedCache.empty(24, 16, H, B, 5, dtype=cache)
+    c.page_table.copy_(torch.randperm(24, generator=torch.Generator().manual_seed(3))[:20].view(B, 5).int())
+    seq = torch.arange(B, device="cuda").int().repeat(56)               # rows of the layer's cache: position-major
+    pos = torch.arange(56, device="cuda").int().repeat_interleave(B)
+    keep = torch.where(pos < torch.tensor(lens, device="cuda").int()[seq.long()], pos, -1)
+    c.write(layer.k_cache.view(56 * B, d), layer.v_cache.view(56 * B, d), seq, keep)
+
+    w = {n: torch.tensor(lw[n], device="cuda") for n in lw}
+    g32 = {n: w[n].float() for n in ("g_q", "g_k")}
+    rot = rt.QkRotate(H, H, "f32", rot_dim=0)
+    rms = lambda u, g: u / torch.sqrt((u * u).mean(-1, keepdim=True) + 1e-6) * g
+    slope_t = torch.tensor(slopes, device="cuda")
+    batch = torch.arange(B, device="cuda").int()
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    worst = 0.0
+    for s in range(steps):
+        xi = torch.tensor(np.stack([x[b, lens[b] + s] for b in range(B)]), device="cuda")
+        u = rms(xi, w["g_attn"])
+        q, kt, vt = ((u @ w[m].T).float() for m in ("w_q", "w_k", "w_v"))
+        q, kt = rot.forward(q, kt, n, g32["g_q"], g32["g_k"])
+        a = c.attend(q.view(B, H, 64), n, k_own=kt.view(B, H, 64), v_own=vt.view(B, H, 64), alibi_slopes=slope_t)
+        h = xi + a.double().view(B, d) @ w["w_o"].T
+        z = h + torch.nn.functional.gelu(rms(h, w["g_mlp"]) @ w["w_up"].T) @ w["w_down"].T
+        uz = rms(z, w["g_kv"])
+        kp, vp = ((uz @ w[m].T).float() for m in ("w_k", "w_v"))
+        _, kp = rot.forward(kp, kp, n, g32["g_q"], g32["g_k"])
+        c.write(kp.view(B, H, 64), vp.view(B, H, 64), batch, n)
+        ref = np.stack([z_ref[b, lens[b] + s] for b in range(B)])
+        worst = max(worst, float((z.cpu().numpy() - ref).__abs__().max() / np.abs(ref).max()))
+        n += 1
+    torch.cuda.synchronize()
+    assert c.status() == rt.RT_OK
+    # fp32: the library's own tolerance for a layer.  e4m3: keys and values off by up to 2^-4 each; the attention averages, the layer adds it to x: the
+    # difference stays below the rounding of a single pair
+    assert worst <= (1e-4 if cache == "f32" else 2.0 ** -4), worst
+
+
+def test_first_calls_may_be_captured():
+    # in a process of its own, where no kernel has run before
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2604_21215_b200 import rt
+c = rt.PagedCache.empty(64, 16, 2, 2, 32, head_dim=128, dtype="e4m3")
+c.page_table.copy_(torch.arange(64).view(2, 32).int())
+n = torch.tensor([300, 17], dtype=torch.int32, device="cuda")
+q, kv = torch.randn(2, 6, 128, device="cuda"), torch.randn(2, 2, 128, device="cuda")
+g, seq = torch.ones(6 * 128, device="cuda"), torch.arange(2, device="cuda").int()
+op = rt.QkRotate(6, 2, "f32", head_dim=128)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+def step():
+    qr, kr = op.forward(q, kv, n, g, g[:256])
+    c.write(kr, kv, seq, n)
+    out = c.attend(qr, n, k_own=kr, v_own=kv)
+    k, v = c.read(seq, n, dtype="f32")
+    return (out, k, v) + op.backward(q, kv, n, qr, kr, g, g[:256])
+with torch.cuda.graph(graph):
+    got = step()
+graph.replay()
+torch.cuda.synchronize()
+want = step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, want)) and c.status() == 0
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
