@@ -298,9 +298,15 @@ def make_config(d_model: int, n_heads: int, d_ff: int, dtype: str = "bf16", sche
 
 # ------------------------------------------------------------------ conveniences on torch tensors
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _tdtype(dtype: str):
@@ -321,9 +327,8 @@ def _require(ok: bool, where: str):
         raise RtError(RT_ERR_INVALID_ARG, where)
 
 
-def _raw_stream(index: int) -> int:
-    """The current stream of a device as a cudaStream_t (torch.cuda.current_stream builds an object for it, 2 us)."""
-    return _torch()._C._cuda_getCurrentRawStream(index)
+def _on_device(torch, index: int) -> bool:
+    return torch._C._cuda_getDevice() == index
 
 
 def _rows(t, heads: int, head_dim: int, n: int, dtype, index: int, where: str) -> tuple:
@@ -590,7 +595,8 @@ class Stack:
 class PagedCache:
     """The pairs of one layer's sequences in pages, over tensors of the caller: k and v [n_pages, n_kv_heads, page_size, head_dim] (float32,
     bfloat16 or float8_e4m3fn, the last with exponents k_exp and v_exp, uint8 [n_pages, n_kv_heads, page_size]) and page_table, int32
-    [n_seqs, max_pages].  Which pages a sequence owns is the caller's to say: it writes the page table.
+    [n_seqs, max_pages].  Which pages a sequence owns is the caller's to say: it writes the page table,
+    in place (the object keeps the tensors that it was made with).
 
     The methods take device tensors, enqueue on the current stream and return; nothing is kept between calls but the status word."""
 
@@ -609,6 +615,7 @@ class PagedCache:
                                _vector(v_exp, n_pages * n_kv * page, torch.uint8, k.device.index, "PagedCache: v_exp"), page_table.data_ptr(),
                                self._status.data_ptr(), n_pages, page, n_kv, hd, code, page_table.shape[0], page_table.shape[1])
         self._index = k.device.index
+        self._ref, self._scale = C.byref(self._c), 1.0 / math.sqrt(hd)
         self._codes = {torch.float32: RT_F32, torch.bfloat16: RT_BF16}
         self._ws_like: dict = {}                       # by number of query heads: one word seen as an array of the workspace's size
         _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, "PagedCache: shape")
@@ -624,34 +631,44 @@ class PagedCache:
         exps = lambda: torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == "e4m3" else None
         return cls(pool(), pool(), torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), exps(), exps())
 
+    # (The methods below are called for every layer and token: checks and arguments are kept to the few microseconds that they need.  Arrays made here
+    # need no check, and torch._C gives the current stream as a number, where torch.cuda.current_stream builds an object for it.)
+
     def write(self, k, v, seq, pos) -> None:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
         seq[r] (int32); a negative position skips the row."""
-        torch, c, dev, n = _torch(), self._c, self._index, k.shape[0]
-        if torch._C._cuda_getDevice() != dev:
+        torch, c, dev, n, t = _torch(), self._c, self._index, k.shape[0], k.dtype
+        if not _on_device(torch, dev):
             with torch.cuda.device(dev):
                 return self.write(k, v, seq, pos)
-        _require(k.dtype in self._codes, "PagedCache.write: k")
-        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, k.dtype, dev, "PagedCache.write: k")
-        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, k.dtype, dev, "PagedCache.write: v")
+        code = self._codes.get(t)
+        _require(code is not None, "PagedCache.write: k")
+        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.write: k")
+        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.write: v")
         sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.write: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.write: pos")
-        _check(rt_cache_write(c, self._codes[k.dtype], kp, vp, ks, vs, sp, pp, n, _raw_stream(dev)), "rt_cache_write")
+        _check(_lib.rt_cache_write(self._ref, code, kp, vp, ks, vs, sp, pp, n, torch._C._cuda_getCurrentRawStream(dev)), "rt_cache_write")
 
     def read(self, seq, pos, dtype: str = "bf16", k=None, v=None):
         """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
         Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
         torch, c, dev, n = _torch(), self._c, self._index, pos.shape[0]
-        if torch._C._cuda_getDevice() != dev:
+        if not _on_device(torch, dev):
             with torch.cuda.device(dev):
                 return self.read(seq, pos, dtype, k, v)
-        t = _tdtype(dtype)
-        shape = (n, c.n_kv_heads, c.head_dim)
-        k = self.k.new_empty(shape, dtype=t) if k is None else k
-        v = self.k.new_empty(shape, dtype=t) if v is None else v
-        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: k")
-        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.read: v")
+        kv, hd, t = c.n_kv_heads, c.head_dim, torch.bfloat16 if dtype == "bf16" else _tdtype(dtype)
+        ks = vs = kv * hd
+        if k is None:
+            k = self.k.new_empty((n, kv, hd), dtype=t)
+            kp = k.data_ptr()
+        else:
+            kp, ks = _rows(k, kv, hd, n, t, dev, "PagedCache.read: k")
+        if v is None:
+            v = self.k.new_empty((n, kv, hd), dtype=t)
+            vp = v.data_ptr()
+        else:
+            vp, vs = _rows(v, kv, hd, n, t, dev, "PagedCache.read: v")
         sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.read: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.read: pos")
-        _check(rt_cache_read(c, self._codes[t], kp, vp, ks, vs, sp, pp, n, _raw_stream(dev)), "rt_cache_read")
+        _check(_lib.rt_cache_read(self._ref, self._codes[t], kp, vp, ks, vs, sp, pp, n, torch._C._cuda_getCurrentRawStream(dev)), "rt_cache_read")
         return k, v
 
     def attend(self, q, lens, k_own=None, v_own=None, scale: Optional[float] = None, alibi_slopes=None, out=None, lse=None):
@@ -660,24 +677,30 @@ class PagedCache:
         [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
         whatever the memory holds)."""
         torch, c, dev = _torch(), self._c, self._index
-        if torch._C._cuda_getDevice() != dev:
+        if not _on_device(torch, dev):
             with torch.cuda.device(dev):
                 return self.attend(q, lens, k_own, v_own, scale, alibi_slopes, out, lse)
-        B, kv, hd = c.n_seqs, c.n_kv_heads, c.head_dim
-        _require(q.dtype in self._codes and q.dim() == 3, "PagedCache.attend: q")
-        H, t = q.shape[1], q.dtype
-        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        B, kv, hd, t = c.n_seqs, c.n_kv_heads, c.head_dim, q.dtype
+        code = self._codes.get(t)
+        _require(code is not None and q.dim() == 3, "PagedCache.attend: q")
+        H = q.shape[1]
         a = RtPagedQuery()
         a.q, a.q_stride = _rows(q, H, hd, B, t, dev, "PagedCache.attend: q")
-        a.out, a.out_stride = _rows(out, H, hd, B, t, dev, "PagedCache.attend: out")
-        _require((k_own is None) == (v_own is None), "PagedCache.attend: k_own, v_own")
-        if k_own is not None:
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            a.out, a.out_stride = out.data_ptr(), H * hd
+        else:
+            a.out, a.out_stride = _rows(out, H, hd, B, t, dev, "PagedCache.attend: out")
+        if k_own is not None or v_own is not None:
+            _require(k_own is not None and v_own is not None, "PagedCache.attend: k_own, v_own")
             a.k_own, a.k_own_stride = _rows(k_own, kv, hd, B, t, dev, "PagedCache.attend: k_own")
             a.v_own, a.v_own_stride = _rows(v_own, kv, hd, B, t, dev, "PagedCache.attend: v_own")
         a.lens = _vector(lens, B, torch.int32, dev, "PagedCache.attend: lens")
-        a.alibi_slopes = _vector(alibi_slopes, H, torch.float32, dev, "PagedCache.attend: alibi_slopes")
-        a.lse = _vector(lse, B * H, torch.float32, dev, "PagedCache.attend: lse")
-        a.dtype, a.n_heads, a.softmax_scale = self._codes[t], H, 1.0 / math.sqrt(hd) if scale is None else scale
+        if alibi_slopes is not None:
+            a.alibi_slopes = _vector(alibi_slopes, H, torch.float32, dev, "PagedCache.attend: alibi_slopes")
+        if lse is not None:
+            a.lse = _vector(lse, B * H, torch.float32, dev, "PagedCache.attend: lse")
+        a.dtype, a.n_heads, a.softmax_scale = code, H, self._scale if scale is None else scale
         like = self._ws_like.get(H)
         if like is None:
             need = rt_paged_attention_workspace_bytes(c, H)
@@ -685,7 +708,8 @@ class PagedCache:
             like = self._ws_like[H] = self._status.expand(need // 4)
         # a workspace of its own for every call: calls on two streams, or two captured graphs, may overlap
         ws = torch.empty_like(like, memory_format=torch.contiguous_format)
-        _check(rt_paged_attention(c, a, ws.data_ptr(), 4 * ws.numel(), _raw_stream(dev)), "rt_paged_attention")
+        _check(_lib.rt_paged_attention(self._ref, C.byref(a), ws.data_ptr(), 4 * like.shape[0], torch._C._cuda_getCurrentRawStream(dev)),
+               "rt_paged_attention")
         return out
 
     def status(self) -> int:
@@ -708,52 +732,69 @@ class QkRotate:
         self._freq = (C.c_double * max(len(freq), 1))(*freq)
         self.cfg = RtRotateConfig({"f32": RT_F32, "bf16": RT_BF16}[dtype], n_heads, n_kv_heads, head_dim, RT_NORM_QK if norm else 0, rms_eps,
                                   rot_dim, {"halves": RT_PAIRS_HALVES, "neighbours": RT_PAIRS_NEIGHBOURS}[pairs], self._freq)
+        self._ref, self._need = C.byref(self.cfg), (-1, 0)      # (rows of the last backward call, bytes of its workspace)
         _require(rt_qk_rotate_backward_workspace_bytes(self.cfg, 1) > 0, "QkRotate: shape")
 
     def _inputs(self, q, k, pos, g_q, g_k):
-        torch, hd, n, t, dev = _torch(), self.head_dim, q.shape[0], self._t, q.get_device()
-        _require(q.is_cuda and (k is not None or self.n_kv_heads == 0), "QkRotate: q, k")
-        qp, qs = _rows(q, self.n_heads, hd, n, t, dev, "QkRotate: q")
-        kp, ks = _rows(k, self.n_kv_heads, hd, n, t, dev, "QkRotate: k") if self.n_kv_heads else (None, 0)
-        return (n, t, dev, qp, qs, kp, ks, _vector(g_q, self.n_heads * hd, t, dev, "QkRotate: g_q"),
-                _vector(g_k, self.n_kv_heads * hd, t, dev, "QkRotate: g_k"), _vector(pos, n, torch.int32, dev, "QkRotate: pos"))
+        torch, H, kv, hd, n, t, dev = _torch(), self.n_heads, self.n_kv_heads, self.head_dim, q.shape[0], self._t, q.get_device()
+        _require(dev >= 0 and (k is not None or kv == 0), "QkRotate: q, k")
+        qp, qs = _rows(q, H, hd, n, t, dev, "QkRotate: q")
+        kp, ks = _rows(k, kv, hd, n, t, dev, "QkRotate: k") if kv else (None, 0)
+        gq = None if g_q is None else _vector(g_q, H * hd, t, dev, "QkRotate: g_q")
+        gk = None if g_k is None or not kv else _vector(g_k, kv * hd, t, dev, "QkRotate: g_k")
+        return n, t, dev, qp, qs, kp, ks, gq, gk, _vector(pos, n, torch.int32, dev, "QkRotate: pos")
 
     def forward(self, q, k, pos, g_q=None, g_k=None, q_out=None, k_out=None):
         """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
         and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
-        torch = _torch()
-        if q.is_cuda and torch._C._cuda_getDevice() != q.get_device():
+        torch, H, kv, hd = _torch(), self.n_heads, self.n_kv_heads, self.head_dim
+        if q.is_cuda and not _on_device(torch, q.get_device()):
             with torch.cuda.device(q.get_device()):
                 return self.forward(q, k, pos, g_q, g_k, q_out, k_out)
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
-        qo, qos = _rows(q_out, self.n_heads, self.head_dim, n, t, dev, "QkRotate.forward: q_out")
-        ko, kos = None, 0
-        if self.n_kv_heads:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
-            ko, kos = _rows(k_out, self.n_kv_heads, self.head_dim, n, t, dev, "QkRotate.forward: k_out")
-        _check(rt_qk_rotate(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, _raw_stream(dev)), "rt_qk_rotate")
+        qos, ko, kos = H * hd, None, kv * hd
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            qo = q_out.data_ptr()
+        else:
+            qo, qos = _rows(q_out, H, hd, n, t, dev, "QkRotate.forward: q_out")
+        if kv and k_out is None:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+            ko = k_out.data_ptr()
+        elif kv:
+            ko, kos = _rows(k_out, kv, hd, n, t, dev, "QkRotate.forward: k_out")
+        _check(_lib.rt_qk_rotate(self._ref, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, torch._C._cuda_getCurrentRawStream(dev)), "rt_qk_rotate")
         return q_out, k_out
 
     def backward(self, q, k, pos, dq_out, dk_out, g_q=None, g_k=None, dq=None, dk=None):
         """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
         gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
-        torch = _torch()
-        if q.is_cuda and torch._C._cuda_getDevice() != q.get_device():
+        torch, H, kv, hd = _torch(), self.n_heads, self.n_kv_heads, self.head_dim
+        if q.is_cuda and not _on_device(torch, q.get_device()):
             with torch.cuda.device(q.get_device()):
                 return self.backward(q, k, pos, dq_out, dk_out, g_q, g_k, dq, dk)
-        f32, hd = torch.float32, self.head_dim
+        f32 = torch.float32
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
-        kn = n * self.n_kv_heads * hd
-        dq = torch.empty_like(dq_out) if dq is None else dq
-        dk = (torch.empty_like(dk_out) if dk is None else dk) if self.n_kv_heads else None
-        dgq = None if g_q is None else torch.empty_like(g_q, dtype=f32)
-        dgk = None if g_k is None or not self.n_kv_heads else torch.empty_like(g_k, dtype=f32)
-        ptr = lambda x: None if x is None else x.data_ptr()
-        ws = torch.empty(rt_qk_rotate_backward_workspace_bytes(self.cfg, n), dtype=torch.uint8, device=q.device)
-        _check(rt_qk_rotate_backward(self.cfg, qp, kp, qs, ks, gq, gk, pp, n, _vector(dq_out, n * self.n_heads * hd, f32, dev, "QkRotate.backward: dq_out"),
-                                     _vector(dk_out, kn, f32, dev, "QkRotate.backward: dk_out") if kn else None,
-                                     _vector(dq, n * self.n_heads * hd, f32, dev, "QkRotate.backward: dq"),
-                                     _vector(dk, kn, f32, dev, "QkRotate.backward: dk") if kn else None, ptr(dgq), ptr(dgk), ws.data_ptr(), ws.numel(),
-                                     _raw_stream(dev)), "rt_qk_rotate_backward")
+        dqo = _vector(dq_out, n * H * hd, f32, dev, "QkRotate.backward: dq_out")
+        if dq is None:
+            dq = torch.empty_like(dq_out)
+            dqp = dq.data_ptr()
+        else:
+            dqp = _vector(dq, n * H * hd, f32, dev, "QkRotate.backward: dq")
+        dko = dkp = dgk = None
+        if kv:
+            dko = _vector(dk_out, n * kv * hd, f32, dev, "QkRotate.backward: dk_out")
+            if dk is None:
+                dk = torch.empty_like(dk_out)
+                dkp = dk.data_ptr()
+            else:
+                dkp = _vector(dk, n * kv * hd, f32, dev, "QkRotate.backward: dk")
+            dgk = None if gk is None else torch.empty_like(g_k, dtype=f32)
+        dgq = None if gq is None else torch.empty_like(g_q, dtype=f32)
+        if self._need[0] != n:
+            self._need = (n, rt_qk_rotate_backward_workspace_bytes(self.cfg, n))
+        ws = dq_out.new_empty(self._need[1] // 4)
+        _check(_lib.rt_qk_rotate_backward(self._ref, qp, kp, qs, ks, gq, gk, pp, n, dqo, dko, dqp, dkp, None if dgq is None else dgq.data_ptr(),
+                                          None if dgk is None else dgk.data_ptr(), ws.data_ptr(), self._need[1],
+                                          torch._C._cuda_getCurrentRawStream(dev)), "rt_qk_rotate_backward")
         return dq, dk, dgq, dgk
