@@ -47,6 +47,14 @@ cudaError_t rotate_backward_launch(int dtype, const RotateParams& p, void* works
 size_t rotate_backward_workspace(int heads, int hd, int rows);
 
 #ifdef __CUDACC__
+// ---- two fp32 numbers in a register pair: sm_100a multiplies and adds them in one instruction
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
 // ---- eight consecutive elements <-> float ----------------------------------------------------
 __device__ __forceinline__ void unpack8(const uint4& a, float (&f)[8]) {
   const unsigned w[4] = {a.x, a.y, a.z, a.w};

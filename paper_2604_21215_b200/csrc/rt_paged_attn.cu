@@ -36,15 +36,15 @@ constexpr float kWeightLog2 = 10.0f;      // fp16 weights lie in [0, 2^10]: thei
 template <typename CT, int HD>
 struct Shape {
   static constexpr int RB = HD * (int)sizeof(CT), NCH = RB / 16;             // bytes and 16-byte chunks of a row
-  static constexpr int KT = HD == 64 && sizeof(CT) < 4 ? 32 : 16;            // positions of a unit (16 of them lie in one page)
-  static constexpr int SUB = KT / 16;
+  static constexpr int KT = HD == 128 || sizeof(CT) == 4 ? 16 : sizeof(CT) == 1 ? 64 : 32;      // positions of a unit
+  static constexpr int SUB = KT / 16;                                        // (sixteens of them lie in one page)
   static constexpr int KV = 2 * KT * RB;
   static constexpr int EXP = sizeof(CT) == 1 ? 2 * KT : 0;
   static constexpr int OUT = kRows * (HD + 2) * 4;                           // a used stage also carries a head's results
   static constexpr int STAGE = ((KV + EXP > OUT ? KV + EXP : OUT) + 127) / 128 * 128;
   // Units of a ring, and blocks of an SM (both limited by the SM's 227 KB, and by 65,536 registers).  Twelve warps an SM hide a unit's chain of products,
   // maxima and exponentials better than eight with a deeper ring; heads of 128 in bf16 need the registers of eight.
-  static constexpr bool SMALL = HD == 64 && sizeof(CT) == 2;
+  static constexpr bool SMALL = HD == 64 && sizeof(CT) <= 2;
   static constexpr int STAGES = KV <= 4096 ? 4 : SMALL ? 2 : 3;
   static constexpr int CTAS = KV <= 4096 || SMALL ? 3 : KV <= 8192 ? 2 : 1;
   static constexpr int SMEM = kWarps * STAGES * STAGE;
@@ -157,20 +157,32 @@ __device__ __forceinline__ void mma_first(float (&c)[4], unsigned a0, unsigned a
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ unsigned pack_h2(float a, float b) {
+__device__ __forceinline__ F2 ex2(F2 x) {
+  float a, b;
+  split(x, a, b);
+  return f2(ex2(a), ex2(b));
+}
+// two numbers rounded to a 16-bit type; take_ leaves what the rounding lost
+__device__ __forceinline__ unsigned round_bf16(F2 x) {
+  float a, b;
+  split(x, a, b);
+  return pack2(a, b);
+}
+__device__ __forceinline__ unsigned round_f16(F2 x) {
+  float a, b;
+  split(x, a, b);
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
 }
-// (a, b) rounded to 16-bit types, and what the rounding left
-__device__ __forceinline__ unsigned take_bf16(float& a, float& b) {
-  const unsigned w = pack2(a, b);
-  a -= __uint_as_float(w << 16); b -= __uint_as_float(w & 0xffff0000u);
+__device__ __forceinline__ unsigned take_bf16(F2& x) {
+  const unsigned w = round_bf16(x);
+  x = add(x, f2(__uint_as_float((w << 16) ^ 0x80000000u), __uint_as_float((w & 0xffff0000u) ^ 0x80000000u)));
   return w;
 }
-__device__ __forceinline__ unsigned take_f16(float& a, float& b) {
-  const unsigned w = pack_h2(a, b);
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-  a -= f.x; b -= f.y;
+__device__ __forceinline__ unsigned take_f16(F2& x) {
+  const unsigned w = round_f16(x);
+  const float2 f = __half22float2(__hneg2(*reinterpret_cast<const __half2*>(&w)));
+  x = add(x, f2(f.x, f.y));
   return w;
 }
 __device__ __forceinline__ unsigned e4m3x2_to_h2(unsigned v) {
@@ -196,7 +208,8 @@ struct Mma {
   static constexpr int KS = HD / 16, NT = S::KT / 8, KPL = S::KT / 4, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
   unsigned q[TERMS][KS][2];
   float o[HD / 8][4];
-  float m, l, mv, q_scale;                 // running maximum (log2 units), this lane's part of the sum, maximum of the scaled weights (F8)
+  float m, mv, q_scale;                    // running maximum (log2 units), that of the scaled weights (F8)
+  F2 l;                                    // this lane's part of the sum
   float slope;
 
   // Where a product of weights and values adds up.  The tensor core cuts what a sum loses instead of rounding it, which over thousands of
@@ -217,7 +230,7 @@ struct Mma {
     const int r = lane >> 2, c = lane & 3;
     const bool in = r < g_in;
     const size_t at = (size_t)b * p.q.q_stride + (size_t)(h0 + (in ? r : 0)) * HD;
-    float x[HD / 4];
+    F2 x[HD / 8];
 #pragma unroll
     for (int i = 0; i < S::NCH / 4; ++i) {
 #pragma unroll
@@ -227,32 +240,36 @@ struct Mma {
         if (p.q.dtype == RT_BF16) load8((const __nv_bfloat16*)p.q.q + d, f);
         else load8((const float*)p.q.q + d, f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[i * E + e + k] = in ? f[k] : 0.f;
+        for (int k = 0; k < 4; ++k) x[(i * E + e) / 2 + k] = f2(in ? f[2 * k] : 0.f, in ? f[2 * k + 1] : 0.f);
       }
     }
     q_scale = p.scale_log2;
     if (F8) {                              // the largest of the row to [2^10, 2^11)
       float a = 0.f;
 #pragma unroll
-      for (int d = 0; d < HD / 4; ++d) a = fmaxf(a, fabsf(x[d]));
+      for (int d = 0; d < HD / 8; ++d) {
+        float y, z;
+        split(x[d], y, z);
+        a = fmaxf(a, fmaxf(fabsf(y), fabsf(z)));
+      }
       a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
       a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
       const int k = min(137 - (int)(__float_as_uint(a) >> 23), 100);       // 10 - floor(log2 a), at least -118
       const float up = __uint_as_float((unsigned)(127 + k) << 23);
 #pragma unroll
-      for (int d = 0; d < HD / 4; ++d) x[d] *= up;
+      for (int d = 0; d < HD / 8; ++d) x[d] = mul(x[d], f2(up, up));
       q_scale *= __uint_as_float((unsigned)(127 - k) << 23);
     }
 #pragma unroll
     for (int t = 0; t < TERMS; ++t)
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        q[t][s][0] = F8 ? take_f16(x[4 * s], x[4 * s + 1]) : take_bf16(x[4 * s], x[4 * s + 1]);
-        q[t][s][1] = F8 ? take_f16(x[4 * s + 2], x[4 * s + 3]) : take_bf16(x[4 * s + 2], x[4 * s + 3]);
+        q[t][s][0] = F8 ? take_f16(x[2 * s]) : take_bf16(x[2 * s]);
+        q[t][s][1] = F8 ? take_f16(x[2 * s + 1]) : take_bf16(x[2 * s + 1]);
       }
     slope = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h0 + (in ? r : 0)) * kLog2e : 0.f;
     m = mv = -INFINITY;
-    l = 0.f;
+    l = f2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
 #pragma unroll
@@ -290,8 +307,8 @@ struct Mma {
         }
       }
     }
-    // scores in log2 units (for F8 also those of the scaled weights), the maximum of the row, weights
-    float a[NT][2], av[F8 ? NT : 1][2], top = m, topv = mv;
+    // scores in log2 units (for F8 also those of the scaled weights), the maximum of the row, weights; two positions at a time
+    F2 a[NT], av[F8 ? NT : 1];
     unsigned ke[KPL / 4], ve[KPL / 4];       // the exponents of this lane's positions
     if (F8) {
 #pragma unroll
@@ -300,53 +317,59 @@ struct Mma {
         ve[y] = reinterpret_cast<const unsigned*>(st + S::KV + S::KT + KPL * c)[y];
       }
     }
+    const F2 scale2 = f2(q_scale, q_scale);
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int j = 2 * t + e;             // of the lane's positions
-        float x = TERMS > 1 ? s[t][e] + s[t][e + 2] : s[t][e];
-        if (F8) {
-          const unsigned kw = ke[j / 4], b = j % 4;
-          x *= q_scale * __uint_as_float(b == 3 ? kw >> 1 & 0x7f800000u : kw << (23 - 8 * b) & 0x7f800000u);
-        } else {
-          x *= q_scale;
-        }
-        a[t][e] = x;
+    for (int t = 0; t < NT; ++t) {           // positions 2 t and 2 t + 1 of the lane's
+      F2 x = f2(s[t][0], s[t][1]);
+      if (TERMS > 1) x = add(x, f2(s[t][2], s[t][3]));
+      if (F8) {
+        const unsigned w = ke[t / 2];
+        const F2 ks = t & 1 ? f2(__uint_as_float(w << 7 & 0x7f800000u), __uint_as_float(w >> 1 & 0x7f800000u))
+                            : f2(__uint_as_float(w << 23 & 0x7f800000u), __uint_as_float(w << 15 & 0x7f800000u));
+        a[t] = mul(x, mul(scale2, ks));
+      } else {
+        a[t] = mul(x, scale2);
       }
+    }
     if (p.q.alibi_slopes) {
       const float far = (float)(j0 + KPL * c - at);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) a[t][e] = fmaf(slope, far + (float)(2 * t + e), a[t][e]);
+      for (int t = 0; t < NT; ++t) a[t] = fma(f2(slope, slope), add(f2(far, far), f2((float)(2 * t), (float)(2 * t + 1))), a[t]);
     }
     if (F8) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {        // 2^23 + exponent - (2^23 + 127)
-          const int j = 2 * t + e;
-          av[F8 ? t : 0][e] = a[t][e] + (__uint_as_float(__byte_perm(ve[j / 4], 0x4b000000u, 0x7550u + j % 4)) - 8388735.f);
-        }
+      for (int t = 0; t < NT; ++t) {         // 2^23 + exponent - (2^23 + 127)
+        const unsigned w = ve[t / 2], sel = 0x7550u + 2 * (t & 1);
+        av[F8 ? t : 0] = add(a[t], add(f2(__uint_as_float(__byte_perm(w, 0x4b000000u, sel)), __uint_as_float(__byte_perm(w, 0x4b000000u, sel + 1))),
+                                       f2(-8388735.f, -8388735.f)));
+      }
     }
     if (live < S::KT || bad) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (KPL * c + 2 * t + e >= live || (bad >> ((KPL * c) / 16) & 1)) {
-            a[t][e] = -INFINITY;
-            if (F8) av[F8 ? t : 0][e] = -INFINITY;
-          }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top = fmaxf(top, a[t][e]);
-        if (F8) topv = fmaxf(topv, av[F8 ? t : 0][e]);
+      for (int t = 0; t < NT; ++t) {
+        const int j = KPL * c + 2 * t;
+        const bool gone = bad >> (j / 16) & 1;
+        const float i0 = gone || j >= live ? -INFINITY : 0.f, i1 = gone || j + 1 >= live ? -INFINITY : 0.f;
+        float x, y;
+        split(a[t], x, y);
+        a[t] = f2(i0 != 0.f ? i0 : x, i1 != 0.f ? i1 : y);
+        if (F8) {
+          split(av[F8 ? t : 0], x, y);
+          av[F8 ? t : 0] = f2(i0 != 0.f ? i0 : x, i1 != 0.f ? i1 : y);
+        }
       }
+    }
+    float top = m, topv = mv;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float x, y;
+      split(a[t], x, y);
+      top = fmaxf(top, fmaxf(x, y));
+      if (F8) {
+        split(av[F8 ? t : 0], x, y);
+        topv = fmaxf(topv, fmaxf(x, y));
+      }
+    }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     if (F8) {
@@ -356,7 +379,7 @@ struct Mma {
     if (__any_sync(0xffffffffu, top > m || (F8 && topv > mv))) {
       const float w = m == -INFINITY ? 0.f : ex2(m - top);
       const float wo = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - topv)) : w;
-      l *= w;
+      l = mul(l, f2(w, w));
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j)
 #pragma unroll
@@ -364,24 +387,24 @@ struct Mma {
       m = top;
       mv = topv;
     }
-    const float ref = m == -INFINITY ? 0.f : m, refv = mv == -INFINITY ? 0.f : mv - kWeightLog2;
+    const float ref = m == -INFINITY ? 0.f : -m, refv = mv == -INFINITY ? 0.f : kWeightLog2 - mv;
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
-      float w[4];                          // positions 4 sub + (0 .. 3) of the lane's
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = 2 * sub + e / 2;
-        w[e] = ex2(a[t][e & 1] - ref);
-        l += w[e];
-        if (F8) w[e] = ex2(av[F8 ? t : 0][e & 1] - refv);
-      }
-      unsigned w0[2], w1[2], w2[2];
+      unsigned w0[2], w1[2], w2[2];          // terms of the weights of positions 4 sub + (0, 1) and (2, 3) of the lane's
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (F8) { w0[h] = take_f16(w[2 * h], w[2 * h + 1]); w1[h] = take_f16(w[2 * h], w[2 * h + 1]); w2[h] = 0; }
-        else {
-          w0[h] = take_bf16(w[2 * h], w[2 * h + 1]); w1[h] = take_bf16(w[2 * h], w[2 * h + 1]);
-          w2[h] = pack2(w[2 * h], w[2 * h + 1]);
+        const int t = 2 * sub + h;
+        F2 w = ex2(add(a[t], f2(ref, ref)));
+        l = add(l, w);
+        if (F8) {
+          w = ex2(add(av[F8 ? t : 0], f2(refv, refv)));
+          w0[h] = take_f16(w);
+          w1[h] = round_f16(w);
+          w2[h] = 0;
+        } else {
+          w0[h] = take_bf16(w);
+          w1[h] = take_bf16(w);
+          w2[h] = round_bf16(w);
         }
       }
       const unsigned char* vt = st + S::KT * S::RB;
@@ -450,8 +473,11 @@ struct Mma {
   __device__ __forceinline__ bool dump(float* out, int g_in, int lane) {
     const int r = lane >> 2, c = lane & 3;
     float all = 0.f;
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    float sum, other;
+    split(l, sum, other);
+    sum += other;
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     const float back = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - m - kWeightLog2)) : 1.f;
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
@@ -463,8 +489,8 @@ struct Mma {
         out[r * HD + d] = y;
         all = fmaf(y, 0.f, all);           // NaN once one is not finite
       }
-    if (c == 0) { out[kRows * HD + 2 * r] = m; out[kRows * HD + 2 * r + 1] = l; }
-    return !__any_sync(0xffffffffu, r < g_in && !(all == 0.f && l < INFINITY));
+    if (c == 0) { out[kRows * HD + 2 * r] = m; out[kRows * HD + 2 * r + 1] = sum; }
+    return !__any_sync(0xffffffffu, r < g_in && !(all == 0.f && sum < INFINITY));
   }
 };
 
@@ -695,12 +721,19 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
           copy16(dst + S::KT * S::RB + value_place<S::NCH, S::KT>(row, ch) * 16, v + i * 512, 16);
         }
       }
-      if (S::EXP && lane < 2 * S::SUB)
-        copy16(dst + S::KV + (lane & 1) * S::KT + (lane >> 1) * 16, e0 + (S::SUB > 1 && lane > 1 ? off[S::SUB - 1] : off[0]) / S::RB, 16);
+      if (S::EXP && lane < 2 * S::SUB) {
+        size_t mine = off[0];
+#pragma unroll
+        for (int s = 1; s < S::SUB; ++s) if (lane >> 1 == s) mine = off[s];
+        copy16(dst + S::KV + (lane & 1) * S::KT + (lane >> 1) * 16, e0 + mine / S::RB, 16);
+      }
     } else {
 #pragma unroll 1
       for (int s = 0; s < S::SUB; ++s) {
-        const int page = s ? pages[S::SUB - 1] : pages[0], js = j + 16 * s;
+        int page = pages[0];
+#pragma unroll
+        for (int t = 1; t < S::SUB; ++t) if (s == t) page = pages[t];
+        const int js = j + 16 * s;
         const bool ok = (unsigned)page < n_pages;
         const int live = ok ? cp.n - js : 0;
         const size_t off = ok ? (size_t)page * page_bytes + (unsigned)((js & in_page) * S::RB) : 0;

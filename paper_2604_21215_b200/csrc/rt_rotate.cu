@@ -26,13 +26,6 @@ __device__ __forceinline__ Lane lane_of(const RotateParams& p, int c) {
   return {4 * c, 4 * c + p.rot / 2};
 }
 
-// two fp32 numbers in a register pair: sm_100a multiplies and adds them in one instruction
-struct F2 { unsigned long long v; };
-__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void split(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-
 // a run of four elements as it lies in memory
 template <typename T> struct Run;
 template <> struct Run<float> {
