@@ -495,70 +495,107 @@ struct Mma {
 };
 
 // ---- fp32 pages: CUDA cores ----------------------------------------------------------------------
-// HD / 4 lanes a row, 128 / HD rows at a time; every such group of lanes has its own running maximum, sum and output, joined at the end.
+// LPK = HD / 4 lanes hold a row, 128 / HD rows lie side by side.  The heads' dot products are added up over the lanes together: each step hands half of
+// the heads to the other half of the lanes, so that a lane ends with the score of one head (G - 1 shuffles and a few, not 4 or 5 for each head) and
+// maxima, exponentials and sums are that head's alone; its weights go to the other lanes one by one for the outputs.
 template <int HD, int G>
 struct Simt {
   using S = Shape<float, HD>;
-  static constexpr int LPK = HD / 4, KPI = 32 / LPK;
-  float q[G][4], o[G][4], m[G], l[G], slope[G];
-  int g_in;
+  static constexpr int LPK = HD / 4, KPI = 32 / LPK, IT = 16 / KPI, PER = LPK / G;      // PER lanes hold the same head's score
+  F2 q[G][2], o[G][2];
+  float m, l, slope;                       // of this lane's head
 
-  __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in_, int lane) {
-    g_in = g_in_;
+  __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in, int lane) {
+    const int c = lane % LPK;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const int h = h0 + min(g, g_in - 1);
-      slope[g] = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h) * kLog2e : 0.f;
-      m[g] = -INFINITY; l[g] = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        q[g][e] = q_at(p.q.dtype, p.q.q, (size_t)b * p.q.q_stride + (size_t)h * HD + (lane % LPK) * 4 + e);
-        o[g][e] = 0.f;
-      }
+      const size_t at = (size_t)b * p.q.q_stride + (size_t)(h0 + min(g, g_in - 1)) * HD + c * 4;
+      q[g][0] = f2(q_at(p.q.dtype, p.q.q, at), q_at(p.q.dtype, p.q.q, at + 1));
+      q[g][1] = f2(q_at(p.q.dtype, p.q.q, at + 2), q_at(p.q.dtype, p.q.q, at + 3));
+      o[g][0] = o[g][1] = f2(0.f, 0.f);
     }
+    slope = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h0 + min(c / PER, g_in - 1)) * kLog2e : 0.f;
+    m = -INFINITY;
+    l = 0.f;
   }
+  // a value of the lane's head from the lane of each head, in turn
+  __device__ __forceinline__ float from_head(float x, int g, int lane) const { return __shfl_sync(0xffffffffu, x, (lane & ~(LPK - 1)) + g * PER); }
+
   __device__ __forceinline__ void unit(const PagedAttnParams& p, const unsigned char* st, int j0, int at, int live, unsigned bad, int lane) {
     const int sub = lane / LPK, c = lane % LPK;
-#pragma unroll 4
-    for (int i = 0; i < 16 / KPI; ++i) {
+    float s[IT], top = m;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
       const int j = i * KPI + sub;
-      const bool ok = j < live && !bad;
       const float4 k = reinterpret_cast<const float4*>(st)[key_place<S::NCH>(j, c)];
-      const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH, S::KT>(j, c)];
+      const F2 k0 = f2(k.x, k.y), k1 = f2(k.z, k.w);
+      float a[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        float a = q[g][0] * k.x + q[g][1] * k.y + q[g][2] * k.z + q[g][3] * k.w;
+        float x, y;
+        split(fma(q[g][1], k1, mul(q[g][0], k0)), x, y);
+        a[g] = x + y;
+      }
 #pragma unroll
-        for (int w = LPK / 2; w; w >>= 1) a += __shfl_xor_sync(0xffffffffu, a, w);
-        a = ok ? a * p.scale_log2 - slope[g] * (float)(at - j0 - j) : -INFINITY;
-        const float mn = fmaxf(m[g], a), ref = mn == -INFINITY ? 0.f : mn;
-        const float w0 = ex2(m[g] - ref), w1 = ex2(a - ref);
-        m[g] = mn;
-        l[g] = l[g] * w0 + w1;
-        o[g][0] = o[g][0] * w0 + w1 * v.x; o[g][1] = o[g][1] * w0 + w1 * v.y;      // (rows that do not count are zeros)
-        o[g][2] = o[g][2] * w0 + w1 * v.z; o[g][3] = o[g][3] * w0 + w1 * v.w;
+      for (int off = LPK / 2, n = G; off; off >>= 1) {
+        if (n > 1) {
+          n >>= 1;
+          const bool upper = (lane & off) != 0;
+#pragma unroll
+          for (int g = 0; g < G / 2; ++g)
+            if (g < n) {
+              const float send = upper ? a[g] : a[g + n], keep = upper ? a[g + n] : a[g];
+              a[g] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+            }
+        } else {
+          a[0] += __shfl_xor_sync(0xffffffffu, a[0], off);
+        }
+      }
+      s[i] = j < live && !bad ? a[0] * p.scale_log2 - slope * (float)(at - j0 - j) : -INFINITY;
+      top = fmaxf(top, s[i]);
+    }
+    if (KPI == 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, LPK));
+    if (__any_sync(0xffffffffu, top > m)) {
+      const float w = m == -INFINITY ? 0.f : ex2(m - top);
+      l *= w;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float x = from_head(w, g, lane);
+        o[g][0] = mul(o[g][0], f2(x, x));
+        o[g][1] = mul(o[g][1], f2(x, x));
+      }
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const float4 v = reinterpret_cast<const float4*>(st + 16 * S::RB)[value_place<S::NCH, S::KT>(i * KPI + sub, c)];      // (rows that do not count are zeros)
+      const F2 v0 = f2(v.x, v.y), v1 = f2(v.z, v.w);
+      const float w = ex2(s[i] - ref);
+      l += w;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float x = G == 1 ? w : from_head(w, g, lane);
+        o[g][0] = fma(f2(x, x), v0, o[g][0]);
+        o[g][1] = fma(f2(x, x), v1, o[g][1]);
       }
     }
   }
-  __device__ __forceinline__ bool dump(float* out, int, int lane) {
+  __device__ __forceinline__ bool dump(float* out, int g_in, int lane) {
+    const int c = lane % LPK;
+    if (KPI == 2) l += __shfl_xor_sync(0xffffffffu, l, LPK);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-#pragma unroll
-      for (int w = LPK; w < 32; w <<= 1) {
-        const float mo = __shfl_xor_sync(0xffffffffu, m[g], w), lo = __shfl_xor_sync(0xffffffffu, l[g], w);
-        const float mn = fmaxf(m[g], mo), ref = mn == -INFINITY ? 0.f : mn;
-        const float w0 = exp2f(m[g] - ref), w1 = exp2f(mo - ref);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[g][e] = o[g][e] * w0 + __shfl_xor_sync(0xffffffffu, o[g][e], w) * w1;
-        l[g] = l[g] * w0 + lo * w1;
-        m[g] = mn;
+      float4 y;
+      split(o[g][0], y.x, y.y);
+      split(o[g][1], y.z, y.w);
+      if (KPI == 2) {
+        y.x += __shfl_xor_sync(0xffffffffu, y.x, LPK); y.y += __shfl_xor_sync(0xffffffffu, y.y, LPK);
+        y.z += __shfl_xor_sync(0xffffffffu, y.z, LPK); y.w += __shfl_xor_sync(0xffffffffu, y.w, LPK);
       }
-      if (lane < LPK && g < g_in) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[g * HD + lane * 4 + e] = o[g][e];
-        if (lane == 0) { out[kRows * HD + 2 * g] = m[g]; out[kRows * HD + 2 * g + 1] = l[g]; }
-      }
+      if (lane < LPK && g < g_in) *reinterpret_cast<float4*>(out + g * HD + c * 4) = y;
     }
+    if (lane < LPK && c % PER == 0 && c / PER < g_in) { out[kRows * HD + 2 * (c / PER)] = m; out[kRows * HD + 2 * (c / PER) + 1] = l; }
     return true;
   }
 };
