@@ -4,6 +4,8 @@
 // every lane's 16 bytes.  So head_dim / 16 lanes hold a row of a head, 16 elements each in two runs of 8 (every access of a warp covers whole 32-byte
 // sectors on both sides), the cache's type is a template argument, the largest magnitude is found on the bit patterns, two bf16 at a time, and a
 // row's place is looked up once for all heads.
+// Measured on one B200, of 6.55 TB/s: 16 prompts of 2020 positions, 16 heads, bf16 into e4m3 37 us (83 %); 8 of 3550 out of e4m3 as bf16 35 us (78 %); bf16 into bf16 76 %, out 86 %; a step of
+// 16 rows 2.9 us (launch, row, page table, place: four trips in a row).
 #include "rt_paged.h"
 
 namespace rt {

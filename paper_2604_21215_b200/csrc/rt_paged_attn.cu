@@ -1,19 +1,25 @@
 // Attention of one new token of every sequence over its cached pairs, in pages.
 //
-// Bound: HBM reads of the cached pairs (each is used once per head that shares it: one flop a byte for bf16, two for e4m3).
+// Bound: HBM reads of the cached pairs (each is used once per head that shares it: one flop a byte for bf16, two for e4m3), if a unit costs few enough instructions
+// (e4m3: about 420 for 64 positions of a head of 64) and warps enough are there to hide its chain of products, maximum, exponentials and products.
+// Measured on one B200, of 6.55 TB/s: 16 sequences of 12 to 33 thousand pairs, 16 heads, e4m3 128 us (93 %); 128 of 1000, bf16 87 us (94 %);
+// 40 of 0.5 to 8 thousand, 16 query heads on 4 heads of 128, bf16 67 us (85 %); 24 of 0 to 4096, 12 heads 32.5 us (74 %: some 7 us of every call are launches, the first
+// trips to memory and the join; one sequence of 1024 takes 7.3 us).
 //
 // Split.  The work of a call is a line of units: sequence by sequence, head of the cache by head, KT positions a unit.  Every warp of the
 // launch takes an equal piece of that line, wherever it begins and ends, so one long sequence among short ones costs no more than its bytes;
 // the pieces follow from the lengths alone, which each block adds up itself (no plan from the host, the lengths may change between
 // replays of a graph).  A warp writes the heads that it holds whole; of a head that it shares with other warps it leaves maximum, sum
-// and output in the workspace, and a second kernel joins them in the order of the positions (the result does not depend on timing).
+// and output in the workspace, and a second kernel joins them in the order of the positions (the result does not depend on timing).  Joining in the warp that
+// comes last, with a counter for each head, was slower: fence, counter and join one after the other end a call 7 us later, the second kernel 3.
 //
 // Stream.  Each warp runs its own ring of STAGES units in shared memory, filled by 16-byte asynchronous copies that run ahead over the ends of heads and
 // sequences.  Rows behind a length and pages that do not exist arrive as zeros, so what lies there never meets a product.
 //
 // Products.  One query row cannot fill a tensor-core tile, but a tile is the cheapest way to use a staged row for all heads that share it:
-// up to 8 query heads are rows 0-7 of the A operand of mma m16n8k16.  Rows 8-15 carry the second term of the same heads' fp32 numbers, split into 16-bit
-// terms; so scores and weights keep at least 22 bits.  Positions and dimensions are permuted so that each operand is one 16-byte load of a
+// up to 8 query heads are rows 0-7 of the A operand of mma m16n8k16 (registers on both sides: with one row of 16 in use and operands read once, tcgen05's
+// shared-memory operands and its accumulators' way through TMEM would cost more than the products).  Rows 8-15 carry the second term of the same heads' fp32 numbers, split
+// into 16-bit terms; so scores and weights keep at least 22 bits.  Positions and dimensions are permuted so that each operand is one 16-byte load of a
 // row (an order of the contraction is free, and so is the order of the output's columns as long as the epilogue knows it): no transposition.
 //   bf16 pages: bf16 products, queries in 1 (bf16) or 3 terms (fp32), weights in 3 terms.
 //   e4m3 pages: codes are exact in fp16; fp16 products, queries (scaled by a power of two) in 1 or 2 terms, weights in 2 terms.  The keys' scales
@@ -42,8 +48,9 @@ struct Shape {
   static constexpr int EXP = sizeof(CT) == 1 ? 2 * KT : 0;
   static constexpr int OUT = kRows * (HD + 2) * 4;                           // a used stage also carries a head's results
   static constexpr int STAGE = ((KV + EXP > OUT ? KV + EXP : OUT) + 127) / 128 * 128;
-  // Units of a ring, and blocks of an SM (both limited by the SM's 227 KB, and by 65,536 registers).  Twelve warps an SM hide a unit's chain of products,
-  // maxima and exponentials better than eight with a deeper ring; heads of 128 in bf16 need the registers of eight.
+  // Units of a ring, and blocks of an SM (both limited by the SM's 227 KB, and by 65,536 registers).  Twelve warps an SM with two units of 8 KB hide a unit's chain
+  // better than eight with three (ragged bf16 batch 32.5 us against 37.9) or twelve and sixteen with units of 4 KB (34.9, 33.1); e4m3 units of 64 positions instead of 32
+  // spread what a unit costs besides its products (128 us against 143).  Heads of 128 in bf16 need the registers of eight warps.
   static constexpr bool SMALL = HD == 64 && sizeof(CT) <= 2;
   static constexpr int STAGES = KV <= 4096 ? 4 : SMALL ? 2 : 3;
   static constexpr int CTAS = KV <= 4096 || SMALL ? 3 : KV <= 8192 ? 2 : 1;
