@@ -1,7 +1,7 @@
 // Attention of one new token of every sequence over its cached pairs, in pages.
 //
 // Bound: HBM reads of the cached pairs (each is used once per head that shares it: one flop a byte for bf16, two for e4m3), if a unit costs few enough instructions
-// (e4m3: about 420 for 64 positions of a head of 64) and warps enough are there to hide its chain of products, maximum, exponentials and products.
+// (e4m3: about 840 for 64 positions of a head of 64) and warps enough are there to hide its chain of products, maximum, exponentials and products.
 // Measured on one B200, of 6.55 TB/s: 16 sequences of 12 to 33 thousand pairs, 16 heads, e4m3 128 us (93 %); 128 of 1000, bf16 87 us (94 %);
 // 40 of 0.5 to 8 thousand, 16 query heads on 4 heads of 128, bf16 67 us (85 %); 24 of 0 to 4096, 12 heads 32.5 us (74 %: some 7 us of every call are launches, the first
 // trips to memory and the join; one sequence of 1024 takes 7.3 us).

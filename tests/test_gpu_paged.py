@@ -143,6 +143,35 @@ def test_attention_of_one_token(shape, dtype, cache):
     assert c.status() == 0
 
 
+@pytest.mark.parametrize("n_seqs,H,kv,cache", [(300, 2, 2, "bf16"), (700, 4, 2, "e4m3"), (1500, 1, 1, "f32")])
+def test_attention_of_large_ragged_batches(n_seqs, H, kv, cache):
+    # several sequences for each thread that adds up the lengths, more heads than the join has blocks, empty and unused rows in between
+    rng = np.random.default_rng(n_seqs)
+    lens = [int(x) for x in rng.choice([-1, 0, 1, 16, 33, 50, 100, 400], n_seqs, p=[0.1, 0.1, 0.1, 0.1, 0.2, 0.2, 0.15, 0.05])]
+    c, ks, vs = make_cache([max(x, 0) for x in lens], kv, 64, 16, cache, seed=n_seqs)
+    q = torch.randn((n_seqs, H, 64), generator=gen(1), device="cuda")
+    ko, vo = (torch.randn((n_seqs, kv, 64), generator=gen(s), device="cuda") for s in (2, 3))
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = torch.full((n_seqs, H, 64), 4.0, device="cuda"), torch.full((n_seqs, H), 4.0, device="cuda")
+    c.attend(q, n, k_own=ko, v_own=vo, out=out, lse=lse)
+    used = n >= 0
+    assert (out[~used] == 4.0).all() and (lse[~used] == 4.0).all()
+    ref = reference(q, ks, vs, lens, ko, vo)
+    check(out[used], lse[used], tuple(x[used] for x in ref), "f32")
+
+
+@pytest.mark.parametrize("cache,lens", [("bf16", [20011]), ("f32", [20011]), ("e4m3", [60001]), ("bf16", [3, 30000, 1, 7])])
+def test_attention_of_one_long_sequence(cache, lens):
+    # one head shared by hundreds of warps
+    c, ks, vs = make_cache(lens, 1, 64, 64, cache, seed=4)
+    q = torch.randn((len(lens), 2, 64), generator=gen(1), device="cuda")
+    lse = torch.empty((len(lens), 2), device="cuda")
+    slopes = torch.tensor([2.0 ** -8, 2.0 ** -12], device="cuda")
+    for sl in (None, slopes):
+        out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), alibi_slopes=sl, lse=lse)
+        check(out, lse, reference(q, ks, vs, lens, slopes=sl), "f32")
+
+
 def test_attention_with_sharp_and_flat_scores():
     # one key far above the others early or late in the sequence (the running maximum moves), all scores equal, a scale of zero
     lens, H, hd = [700, 700, 300], 2, 64
@@ -329,6 +358,37 @@ def test_rows_in_the_storage_types(dtype, cache):
     assert torch.equal(kr, k.to(TYPES[cache]).to(TYPES[dtype])) and torch.equal(vr, v.to(TYPES[cache]).to(TYPES[dtype]))
 
 
+@pytest.mark.parametrize("dtype,cache", [("f32", "e4m3"), ("bf16", "bf16"), ("bf16", "e4m3"), ("f32", "f32")])
+@pytest.mark.parametrize("rows,kv,hd", [(5003, 1, 64), (4000, 3, 64), (3001, 16, 64), (2500, 5, 128)])
+def test_many_rows(rows, kv, hd, dtype, cache):
+    # several rows a warp, some of them not in use, caches of few and of many heads
+    rt = rt_module()
+    B, page = 7, 32
+    per = -(-rows // B)
+    pages = -(-per // page)
+    c = rt.PagedCache.empty(B * pages, page, kv, B, pages, head_dim=hd, dtype=cache)
+    c.page_table.copy_(torch.randperm(B * pages, generator=torch.Generator().manual_seed(1)).view(B, pages).int())
+    order = torch.randperm(B * per, generator=torch.Generator().manual_seed(2))[:rows].cuda()
+    seq, pos = (order // per).int(), (order % per).int()
+    k, v = (torch.randn((rows, kv, hd), generator=gen(s), device="cuda").to(TYPES[dtype]) for s in (1, 2))
+    skip = torch.rand(rows, generator=gen(3), device="cuda") < 0.2
+    c.write(k, v, seq, torch.where(skip, -1, pos))
+    kr, vr = (torch.full((rows, kv, hd), 6.0, device="cuda") for _ in range(2))
+    c.read(seq, torch.where(skip, -1, pos), dtype="f32", k=kr, v=vr)
+    torch.cuda.synchronize()
+    assert c.status() == 0
+    for got, x in ((kr, k), (vr, v)):
+        assert (got[skip] == 6.0).all()
+        if cache == "e4m3":
+            want, e = quantised(x[~skip])
+            want = (want * 2.0 ** (e.double()[..., None] - 127)).float().cuda()
+        else:
+            want = x[~skip].to(TYPES[cache]).float()
+        assert torch.equal(got[~skip], want)
+    kr, vr = c.read(seq[skip], pos[skip], dtype="f32")                  # what was skipped is not there
+    assert (kr == 0).all() and (vr == 0).all()
+
+
 def test_places_beyond_32_bits():
     # a pool of more than 2^32 bytes and 2^31 values: its last pages hold what was written there
     rt = rt_module()
@@ -415,6 +475,13 @@ ROTATIONS = [  # rows, heads, kv, hd, rot, pairs, norm, gains
     (40, 2, 0, 64, 64, "halves", True, True),
     (1001, 8, 1, 64, 0, "halves", True, True),
     (500, 6, 3, 64, 48, "halves", True, True),
+    # more rows than the GPU holds warps, with heads that fill batches of four, three, two and one, and none
+    (5000, 16, 16, 64, 64, "halves", True, True),
+    (4001, 12, 4, 64, 64, "neighbours", True, True),
+    (9001, 8, 8, 64, 32, "halves", True, False),
+    (3700, 5, 3, 64, 64, "halves", True, True),
+    (4500, 2, 6, 128, 128, "halves", True, True),
+    (20000, 2, 1, 64, 64, "halves", True, True),
 ]
 
 
@@ -453,19 +520,19 @@ def test_rotation_of_normed_queries_and_keys(case, dtype):
 
 
 def test_rotation_in_place_and_rows_not_in_use():
-    case = (50, 4, 2, 64, 64, "halves", True, True)
-    for dtype in ("f32", "bf16"):
-        op, q, k, pos, gq, gk, _ = rotation(case, dtype, seed=3)
-        qo, ko = op.forward(q, k, pos, gq, gk)
-        pos2 = pos.clone()
-        pos2[[3, 49]] = -1
-        q2, k2 = q.clone(), k.clone()
-        a, b = op.forward(q2, k2, pos2, gq, gk, q_out=q2, k_out=k2)
-        assert a is q2 and b is k2
-        for got, ref, x in ((q2, qo, q), (k2, ko, k)):
-            want = ref.clone()
-            want[[3, 49]] = x[[3, 49]]
-            assert torch.equal(got, want)
+    for case in ((50, 4, 2, 64, 64, "halves", True, True), (6000, 16, 16, 64, 64, "neighbours", True, True), (4000, 12, 3, 64, 64, "halves", True, True)):
+        for dtype in ("f32", "bf16"):
+            op, q, k, pos, gq, gk, _ = rotation(case, dtype, seed=3)
+            qo, ko = op.forward(q, k, pos, gq, gk)
+            skip = torch.rand(case[0], generator=gen(5), device="cuda") < 0.3
+            pos2 = torch.where(skip, -1, pos)
+            q2, k2 = q.clone(), k.clone()
+            a, b = op.forward(q2, k2, pos2, gq, gk, q_out=q2, k_out=k2)
+            assert a is q2 and b is k2
+            for got, ref, x in ((q2, qo, q), (k2, ko, k)):
+                want = ref.clone()
+                want[skip] = x[skip]
+                assert torch.equal(got, want)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
