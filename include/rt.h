@@ -304,8 +304,8 @@ rt_status rt_cache_read(const rt_paged_cache *cache, int32_t dtype, void *k, voi
  * one, as in an ordinary decoder):
  *   a_j = softmax_scale <q, k_j> - alibi_slopes[h] (p - j),  p = lens[b] with an own pair (at distance 0), else lens[b] - 1
  *   out = sum_j e^{a_j} v_j / sum_j e^{a_j},   lse = log sum_j e^{a_j}
- * A sequence without any pair gets out = 0 and lse = -infinity.  All arithmetic is fp32 or as good (32-bit softmax statistics
- * and sums, queries and weights to at least 2^-20); `out` is rounded once.  out must not overlap q.
+ * A sequence without any pair gets out = 0 and lse = -infinity.  All arithmetic is fp32 or as good: softmax statistics and
+ * sums in fp32, queries to 2^-22 of a row's largest, weights to 2^-20 (RT_E4M3: and to 2^-40 of the largest weight times value scale).  `out` is rounded once.  out must not overlap q.
  * The work is split evenly over the GPU whatever the lengths are; the result does not depend on timing. */
 typedef struct {
   const void *q;                   /* [n_seqs, n_heads, head_dim] of `dtype` */

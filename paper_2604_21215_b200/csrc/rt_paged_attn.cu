@@ -36,7 +36,7 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 8;      // warps of a block; query heads of a unit
 constexpr int kSms = 148;
-constexpr float kWeightLog2 = 10.0f;      // fp16 weights lie in [0, 2^10]: their second term keeps 2^-35 of the largest
+constexpr float kWeightLog2 = 15.0f;      // fp16 weights lie in [0, 2^15]: their two terms keep 2^-40 of the largest
 
 // ---- shapes ------------------------------------------------------------------------------------
 template <typename CT, int HD>

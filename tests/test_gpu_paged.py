@@ -189,6 +189,28 @@ def test_attention_with_sharp_and_flat_scores():
         check(c.attend(q, n, scale=scale, lse=lse), lse, reference(q, ks, vs, lens, scale=scale), "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("order", [1, -1])
+def test_attention_over_rows_of_very_different_scales(dtype, order):
+    # 8-bit pages whose rows span 2^-20 to 2^20, growing or shrinking along the sequence, weighted towards either end
+    rt = rt_module()
+    B, H, n = 3, 2, 500
+    c = rt.PagedCache.empty(B * 32, 16, H, B, 32, dtype="e4m3")
+    c.page_table.copy_(torch.arange(B * 32).view(B, 32).int())
+    seq, pos = torch.arange(B, device="cuda").int().repeat_interleave(n), torch.arange(n, device="cuda").int().repeat(B)
+    grow = 2.0 ** (order * (torch.arange(n, device="cuda", dtype=torch.float64) / n * 40 - 20)).float().repeat(B)[:, None, None]
+    k = torch.randn((B * n, H, 64), generator=gen(1), device="cuda") * torch.exp2(torch.randint(-3, 2, (B * n, H, 1), generator=gen(5), device="cuda").float())
+    v = torch.randn((B * n, H, 64), generator=gen(2), device="cuda") * grow
+    c.write(k, v, seq, pos)
+    k, v = (x.double().split([n] * B) for x in c.read(seq, pos, dtype="f32"))
+    q = torch.randn((B, H, 64), generator=gen(3), device="cuda").to(TYPES[dtype])
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    for slopes in (None, torch.tensor([0.03, -0.03], device="cuda"), torch.tensor([0.2, 2.0], device="cuda")):
+        lse = torch.empty((B, H), device="cuda")
+        out = c.attend(q, lens, alibi_slopes=slopes, lse=lse)
+        check(out, lse, reference(q, k, v, [n] * B, slopes=slopes), dtype)
+
+
 def test_infinities_and_nan_count_where_they_are_attended_to():
     # a NaN key or value shows in its own head and sequence only; an infinite value as itself; places that are not attended to never show
     for cache in ("f32", "bf16"):
