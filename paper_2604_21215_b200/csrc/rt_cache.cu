@@ -113,7 +113,7 @@ template <int LPR> struct Held<__nv_fp8_e4m3, LPR> {
 // A warp takes the keys or the values of rows_per consecutive rows (at most 32).  Its lanes look their places up together, one row each: the chain row ->
 // page table -> place costs two trips to memory however many rows there are.  Then it goes through the rows' heads, the next loads always under way.
 template <typename T, typename CT, int LPR, bool WRITE>
-__global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_constant__ CacheRowsParams p, int rows_per) {
+__global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_constant__ CacheRowsParams p, int rows_per, unsigned magic) {
   constexpr int HPW = 32 / LPR, HD = LPR * 16;                     // heads side by side in a warp
   constexpr int AHEAD = sizeof(T) == 4 && WRITE ? 1 : 2;           // passes over the heads in flight, and as many on their way
   const int lane = threadIdx.x & 31, c = lane % LPR, hl = lane / LPR, n_kv = p.c.n_kv_heads;
@@ -140,10 +140,11 @@ __global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_co
   // The rows' heads in one line, HPW side by side: head y % n_kv of row y / n_kv.  (Lanes behind the end repeat the last one for the shuffles; rows that are
   // not in use are read from place 0, which is there, and left.)
   const int total = n * n_kv;
+  auto row_of = [&](int y) { return magic ? (int)__umulhi((unsigned)y, magic) : y / n_kv; };
   auto load = [&](Buffer& b, int y0) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int y = min(y0 + u * HPW + hl, total - 1), i = y / n_kv, h = y - i * n_kv;
+      const int y = min(y0 + u * HPW + hl, total - 1), i = row_of(y), h = y - i * n_kv;
       if constexpr (WRITE) {
         const T* from = in + (size_t)i * stride + h * HD;
         b.x[u][0].load(from + c * 8);
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 3) cache_rows_kernel(const __grid_co
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       if (y0 + u * HPW >= total) break;
-      const int y = y0 + u * HPW + hl, yc = min(y, total - 1), i = yc / n_kv, h = yc - i * n_kv;
+      const int y = y0 + u * HPW + hl, yc = min(y, total - 1), i = row_of(yc), h = yc - i * n_kv;
       const long long row0 = __shfl_sync(0xffffffffu, place, i);
       const bool ok = y < total && row0 >= 0;
       if constexpr (WRITE) {
@@ -186,8 +187,10 @@ cudaError_t launch(const CacheRowsParams& p, cudaStream_t s) {
   const int rows_per = (int)min(32LL, max(1LL, ((long long)p.rows * 2 + 148 * 24 - 1) / (148 * 24)));
   const long long warps = ((long long)p.rows + rows_per - 1) / rows_per * 2;
   const dim3 grid((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32)));
-  if (p.c.head_dim == 64) cache_rows_kernel<T, CT, 4, WRITE><<<grid, kThreads, 0, s>>>(p, rows_per);
-  else cache_rows_kernel<T, CT, 8, WRITE><<<grid, kThreads, 0, s>>>(p, rows_per);
+  // ceil(2^32 / n_kv): y / n_kv is the high word of y * magic while y * (magic * n_kv - 2^32) < 2^32, and y < 32 n_kv, that factor < n_kv
+  const unsigned n_kv = (unsigned)p.c.n_kv_heads, magic = n_kv > 1 && n_kv < 8192 ? (unsigned)((0x100000000ull + n_kv - 1) / n_kv) : 0u;
+  if (p.c.head_dim == 64) cache_rows_kernel<T, CT, 4, WRITE><<<grid, kThreads, 0, s>>>(p, rows_per, magic);
+  else cache_rows_kernel<T, CT, 8, WRITE><<<grid, kThreads, 0, s>>>(p, rows_per, magic);
   return cudaGetLastError();
 }
 template <typename T, bool WRITE>

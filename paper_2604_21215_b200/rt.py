@@ -717,6 +717,9 @@ class PagedCache:
         with _torch().cuda.device(self.device):
             return rt_get_status(self._status.data_ptr())
 
+    def clear_status(self) -> None:
+        self._status.zero_()
+
 
 class QkRotate:
     """qkRMS of queries and keys for each head and the rotation by the position, for one layer's shapes.  The angle of pair i at position

@@ -264,7 +264,7 @@ def test_pages_and_lengths_that_do_not_exist():
         torch.cuda.synchronize()
         assert c.status() == rt.RT_ERR_INVALID_ARG
         c.page_table[1, 3] = old
-        c._status.zero_()
+        c.clear_status()
         cut = lambda x: [x[0], torch.cat((x[1][:48], x[1][64:])), x[2]]        # the pairs of that page have no weight
         check(out, lse, reference(q, cut(ks), cut(vs), lens), "f32")
     # a length beyond the table is cut to it
