@@ -103,34 +103,26 @@ struct Turn {
   }
 };
 
-// Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair; the turns are reduced in 64 bits, so that far
-// positions keep their angles.  All lanes of the warp call.
+// Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair through 512 bytes of shared memory of the warp's own (two loads a lane,
+// where shuffles would be 8 or 16); the turns are reduced in 64 bits, so that far positions keep their angles.  All lanes of the warp call.
+struct Angles { float cos[64], sin[64]; };
 template <int LPR>
-__device__ __forceinline__ Turn angles(const RotateParams& p, int pos, int lane) {
-  constexpr int PER = LPR / 8;
-  float co[PER], si[PER];
+__device__ __forceinline__ Turn angles(const RotateParams& p, int pos, int lane, Angles& buf) {
+  __syncwarp();                                                        // (what was there is read)
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    co[k] = 1.f; si[k] = 0.f;
+  for (int k = 0; k < LPR / 8; ++k) {
+    float co = 1.f, si = 0.f;
     const int n = lane + 32 * k;
     if (2 * n < p.rot) {
       const double t = (double)pos * p.turns[n];
-      sincospif((float)(2.0 * (t - rint(t))), &si[k], &co[k]);
+      sincospif((float)(2.0 * (t - rint(t))), &si, &co);
     }
+    buf.cos[n] = co;
+    buf.sin[n] = si;
   }
-  const int c = lane % LPR;
-  float cs[4], sn[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int from = (4 * c + i) & 31;
-    cs[i] = __shfl_sync(0xffffffffu, co[0], from);
-    sn[i] = __shfl_sync(0xffffffffu, si[0], from);
-    if (PER == 2) {
-      const float c1 = __shfl_sync(0xffffffffu, co[PER - 1], from), s1 = __shfl_sync(0xffffffffu, si[PER - 1], from);
-      if (4 * c + i >= 32) { cs[i] = c1; sn[i] = s1; }
-    }
-  }
-  return {{f2(cs[0], cs[1]), f2(cs[2], cs[3])}, {f2(sn[0], sn[1]), f2(sn[2], sn[3])}, {f2(-sn[0], -sn[1]), f2(-sn[2], -sn[3])}};
+  __syncwarp();
+  const float4 c = reinterpret_cast<const float4*>(buf.cos)[lane % LPR], s = reinterpret_cast<const float4*>(buf.sin)[lane % LPR];
+  return {{f2(c.x, c.y), f2(c.z, c.w)}, {f2(s.x, s.y), f2(s.z, s.w)}, {f2(-s.x, -s.y), f2(-s.z, -s.w)}};
 }
 
 // The heads of a launch in block rows of the grid: heads_per of the queries' heads each in the first y_q of them, then heads_per of the keys' heads each.  All heads
@@ -148,6 +140,8 @@ constexpr int kBlocks = 3;      // of an SM, by registers
 template <typename T, int LPR, bool NEIGHBOURS, int AHEAD, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per, int y_q) {
   constexpr int HPW = 32 / LPR, HD = LPR * 8, BATCH = HPW * AHEAD;
+  __shared__ __align__(16) Angles bufs[kThreads / 32];
+  Angles& buf = bufs[threadIdx.x >> 5];
   const int lane = threadIdx.x & 31, hl = lane / LPR;
   const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
   const Part part = part_of(p, blockIdx.y, heads_per, y_q);
@@ -175,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
     for (int u = 0; u < AHEAD; ++u) gr[u].load(g + at(first, u), l);
   }
   load(x, row, h0);
-  Turn turn = angles<LPR>(p, pos, lane);
+  Turn turn = angles<LPR>(p, pos, lane, buf);
   while (true) {
     const bool row_ends = h0 + BATCH >= last;
     const unsigned nr = row_ends ? row + warps : row;
@@ -217,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
     if (!more) break;
     if (row_ends) {
       pos = next_pos;
-      turn = angles<LPR>(p, pos, lane);
+      turn = angles<LPR>(p, pos, lane, buf);
     }
     row = nr;
     h0 = nh;
@@ -231,7 +225,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
 template <typename T, int LPR, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
   constexpr int HPW = 32 / LPR, HD = LPR * 8, ROWS = kThreads / 32, AHEAD = 1;
-  __shared__ float red[ROWS][HPW * HD];
+  __shared__ __align__(16) float red[ROWS][HPW * HD];
+  __shared__ __align__(16) Angles bufs[ROWS];
+  Angles& buf = bufs[threadIdx.x >> 5];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPR, hl = lane / LPR;
   const Lane l = lane_of<NEIGHBOURS>(p, c);
   const int heads = p.n_heads + p.n_kv, hh = blockIdx.y * HPW + hl;
@@ -267,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __gr
     for (int u = 0; u < AHEAD; ++u) {
       const long long row = rb + u * ROWS;
       if (row >= r1 || pos[u] < 0) continue;
-      const Turn turn = angles<LPR>(p, pos[u], lane);
+      const Turn turn = angles<LPR>(p, pos[u], lane, buf);
       Pairs w = turn.back(sides<NEIGHBOURS>(d[u]));
       if (p.norm) {
         Pairs y = sides<NEIGHBOURS>(x[u]);
