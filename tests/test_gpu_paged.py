@@ -119,11 +119,12 @@ SHAPES = [  # lens, heads, kv, hd, page
 ]
 
 
+@pytest.mark.parametrize("room", ["little", "much"])                    # positions that the page table could hold
 @pytest.mark.parametrize("shape", SHAPES)
 @pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "e4m3"), ("f32", "e4m3"), ("f32", "bf16"), ("bf16", "f32")])
-def test_attention_of_one_token(shape, dtype, cache):
+def test_attention_of_one_token(shape, dtype, cache, room):
     lens, H, kv, hd, page = shape
-    c, ks, vs = make_cache(lens, kv, hd, page, cache, seed=len(lens) * hd + H)
+    c, ks, vs = make_cache(lens, kv, hd, page, cache, seed=len(lens) * hd + H, slack=1 if room == "little" else 40000 // page)
     g = gen(5)
     t, B = TYPES[dtype], len(lens)
     q = torch.randn((B, H, hd), generator=g, device="cuda").to(t)
@@ -172,10 +173,11 @@ def test_attention_of_one_long_sequence(cache, lens):
         check(out, lse, reference(q, ks, vs, lens, slopes=sl), "f32")
 
 
-def test_attention_with_sharp_and_flat_scores():
+@pytest.mark.parametrize("slack", [1, 4000])
+def test_attention_with_sharp_and_flat_scores(slack):
     # one key far above the others early or late in the sequence (the running maximum moves), all scores equal, a scale of zero
     lens, H, hd = [700, 700, 300], 2, 64
-    c, ks, vs = make_cache(lens, H, hd, 16, "f32", seed=3)
+    c, ks, vs = make_cache(lens, H, hd, 16, "f32", seed=3, slack=slack)
     q = torch.randn((3, H, hd), generator=gen(1), device="cuda")
     n = torch.tensor(lens, dtype=torch.int32, device="cuda")
     seq, pos = torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.tensor([2, 690], dtype=torch.int32, device="cuda")
@@ -211,10 +213,11 @@ def test_attention_over_rows_of_very_different_scales(dtype, order):
         check(out, lse, reference(q, k, v, [n] * B, slopes=slopes), dtype)
 
 
-def test_infinities_and_nan_count_where_they_are_attended_to():
+@pytest.mark.parametrize("slack", [1, 4000])
+def test_infinities_and_nan_count_where_they_are_attended_to(slack):
     # a NaN key or value shows in its own head and sequence only; an infinite value as itself; places that are not attended to never show
     for cache in ("f32", "bf16"):
-        c, ks, vs = make_cache([40, 40, 40], 2, 64, 16, cache, seed=9)
+        c, ks, vs = make_cache([40, 40, 40], 2, 64, 16, cache, seed=9, slack=slack)
         n = torch.tensor([40, 40, 39], dtype=torch.int32, device="cuda")
         place = lambda b, j: (int(c.page_table[b, j // 16]), j % 16)
         p, o = place(0, 20)
@@ -230,11 +233,12 @@ def test_infinities_and_nan_count_where_they_are_attended_to():
         assert torch.isfinite(out[2]).all()
 
 
-def test_rows_not_in_use_stay_and_strided_rows_are_taken():
+@pytest.mark.parametrize("slack", [1, 4000])
+def test_rows_not_in_use_stay_and_strided_rows_are_taken(slack):
     lens, H, kv, hd = [33, -1, 50, -5], 4, 2, 64
     for cache in ("bf16", "f32"):
         t = TYPES[cache]
-        c, ks, vs = make_cache([33, 0, 50, 0], kv, hd, 16, cache, seed=2)
+        c, ks, vs = make_cache([33, 0, 50, 0], kv, hd, 16, cache, seed=2, slack=slack)
         wide = torch.randn((4, (H + 2 * kv) * hd + 16), generator=gen(3), device="cuda").to(t)        # q | k | v | padding
         q, ko, vo = (wide[:, a * hd:b * hd].view(4, -1, hd) for a, b in ((0, H), (H, H + kv), (H + kv, H + 2 * kv)))
         big = torch.full((4, 2 * H * hd), 3.0, device="cuda", dtype=t)
@@ -247,20 +251,26 @@ def test_rows_not_in_use_stay_and_strided_rows_are_taken():
         check(out[keep], lse[keep], tuple(x[keep] for x in ref), cache)
 
 
-def test_pages_and_lengths_that_do_not_exist():
+@pytest.mark.parametrize("cache,more", [("f32", 0), ("f32", 90), ("bf16", 0), ("bf16", 90)])
+def test_pages_and_lengths_that_do_not_exist(cache, more):
+    # (more: sequences behind these)
     rt = rt_module()
     lens = [70, 200, 64]
-    c, ks, vs = make_cache(lens, 2, 64, 16, "f32", seed=6, slack=0)
+    c, ks, vs = make_cache(lens + [1] * more, 2, 64, 16, cache, seed=6, slack=0)
+    run = lambda q, n, lse=None: c.attend(torch.cat((q, q[:1].expand(more, -1, -1))), torch.cat((n, torch.ones(more, dtype=torch.int32, device="cuda"))),
+                                          lse=None if lse is None else big)[:3]
+    big = torch.empty((3 + more, 2), device="cuda")
     q = torch.randn((3, 2, 64), generator=gen(4), device="cuda")
     n = torch.tensor(lens, dtype=torch.int32, device="cuda")
-    c.attend(q, n)
+    run(q, n)
     torch.cuda.synchronize()
     assert c.status() == rt.RT_OK
+    ks, vs = ks[:3], vs[:3]
     for bad in (-1, c.k.shape[0], 2 ** 31 - 1, -2 ** 31):
         old = int(c.page_table[1, 3])
         c.page_table[1, 3] = bad
-        lse = torch.empty((3, 2), device="cuda")
-        out = c.attend(q, n, lse=lse)
+        out = run(q, n, big)
+        lse = big[:3]
         torch.cuda.synchronize()
         assert c.status() == rt.RT_ERR_INVALID_ARG
         c.page_table[1, 3] = old
@@ -272,9 +282,9 @@ def test_pages_and_lengths_that_do_not_exist():
     full = c.page_table.shape[1] * 16
     assert full == 208
     pos = torch.arange(200, 208, dtype=torch.int32, device="cuda")
-    kx = torch.randn((8, 2, 64), generator=gen(8), device="cuda")
+    kx = torch.randn((8, 2, 64), generator=gen(8), device="cuda").bfloat16().float()
     c.write(kx, kx, torch.ones_like(pos), pos)
-    out = c.attend(q, long)
+    out = run(q, long)
     torch.cuda.synchronize()
     assert c.status() == rt.RT_ERR_INVALID_ARG
     ref = reference(q, [ks[0], torch.cat((ks[1], kx.double())), ks[2]], [vs[0], torch.cat((vs[1], kx.double())), vs[2]], lens)
@@ -431,10 +441,10 @@ def test_places_beyond_32_bits():
     check(out, None, reference(q, cut(k), cut(v), lens), "bf16")
 
 
-def test_attention_is_the_same_on_every_run_stream_and_replay():
-    rt = rt_module()
+@pytest.mark.parametrize("slack", [1, 4000])
+def test_attention_is_the_same_on_every_run_stream_and_replay(slack):
     lens, H = [3000, 1, 0, 517, 64, 2048], 4
-    c, ks, vs = make_cache(lens, 2, 64, 16, "bf16", seed=8)
+    c, ks, vs = make_cache(lens, 2, 64, 16, "bf16", seed=8, slack=slack)
     q = torch.randn((6, H, 64), generator=gen(4), device="cuda").bfloat16()
     n = torch.tensor(lens, dtype=torch.int32, device="cuda")
     first = c.attend(q, n)
