@@ -4,8 +4,8 @@
 // two loads of 4 elements, so the rotation needs no exchange and the norm a few shuffles.  Dimensions that are not rotated make pairs too, with an angle
 // of zero.  A warp takes the heads of one row side by side and one after the other: its lanes form the row's angles once, one or two each.  All products are paired fp32
 // instructions: at 6.5 TB/s an SM has 1370 issue slots for a row of 16 + 16 heads in bf16, and the pass takes 930.
-// Measured on one B200, of 6.55 TB/s: 8 x 4000 rows of 16 + 16 heads of 64 with gains, bf16 51 us (79 %), fp32 90 %; gradients 110 us (92 %).  Heads of 128, whose rows carry twice the
-// angles for as many bytes, 62 and 60 %; 16 query and 4 key heads 50 and 68 %.
+// Measured on one B200, of 6.55 TB/s: 8 x 4000 rows of 16 + 16 heads of 64 with gains, bf16 50 us (81 %), fp32 90 %; gradients 111 us (92 %).  Heads of 128, whose rows carry twice the
+// angles for as many bytes, 65 and 62 %; 16 query and 4 key heads 53 and 67 %.
 #include "rt_paged.h"
 
 namespace rt {
