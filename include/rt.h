@@ -275,7 +275,8 @@ rt_status rt_layer_backward(const rt_config *cfg, const rt_layer_weights *w, con
  *    read or written through it (rt_paged_attention: its pairs get no weight, and a length is cut to max_pages * page_size), and
  *    *status becomes RT_ERR_INVALID_ARG.  No call ever clears that word: the caller zeroes it once and
  *    reads it with rt_get_status.
- *  - The entries of the page table behind a sequence's last page are never read, nor are positions behind its length.
+ *  - The entries of the page table behind a sequence's last page are never used, positions behind its length never read.
+ *  - Outputs overlap neither one another nor inputs, but where an entry point says so (RT_ERR_INVALID_ARG where that shows from addresses and strides).
  *  - Strides are in elements, between the rows of consecutive tokens; a token's heads are contiguous.  Rows begin
  *    at multiples of 16 bytes and do not overlap.  Index arrays and fp32 vectors (lens, lse, slopes) need 4-byte alignment only.
  *  - The pointers belong to the device that is current. */
@@ -305,7 +306,8 @@ rt_status rt_cache_read(const rt_paged_cache *cache, int32_t dtype, void *k, voi
  *   a_j = softmax_scale <q, k_j> - alibi_slopes[h] (p - j),  p = lens[b] with an own pair (at distance 0), else lens[b] - 1
  *   out = sum_j e^{a_j} v_j / sum_j e^{a_j},   lse = log sum_j e^{a_j}
  * A sequence without any pair gets out = 0 and lse = -infinity.  All arithmetic is fp32 or as good: softmax statistics and
- * sums in fp32, queries to 2^-22 of a row's largest, weights to 2^-20 (RT_E4M3: and to 2^-40 of the largest weight times value scale).  `out` is rounded once.  out must not overlap q.
+ * sums in fp32, queries to 2^-22 of a row's largest, weights to 2^-20 (RT_E4M3: and to 2^-40 of the largest weight times
+ * value scale).  `out` is rounded once.
  * The work is split evenly over the GPU whatever the lengths are; the result does not depend on timing. */
 typedef struct {
   const void *q;                   /* [n_seqs, n_heads, head_dim] of `dtype` */

@@ -38,6 +38,20 @@ bool rows_ok(const void* p, int dtype, long long stride, long long row, long lon
   return rows == 1 || (stride >= row && stride <= INT64_MAX / 16 / rows && stride * esize(dtype) % 16 == 0);
 }
 
+// Whether two arrays of such rows share bytes.  Rows of one stride may lie in turn in one array (queries, keys and values of a projection); rows of two strides are
+// taken to overlap only where the arrays begin at the same place.
+bool rows_overlap(const void* a, int dtype_a, long long stride_a, long long row_a, const void* b, int dtype_b, long long stride_b, long long row_b, long long rows) {
+  if (rows == 0) return false;
+  const long long ra = row_a * esize(dtype_a), rb = row_b * esize(dtype_b), sa = rows > 1 ? stride_a * esize(dtype_a) : ra, sb = rows > 1 ? stride_b * esize(dtype_b) : rb;
+  const intptr_t pa = reinterpret_cast<intptr_t>(a), pb = reinterpret_cast<intptr_t>(b);
+  if (pa >= pb + (rows - 1) * sb + rb || pb >= pa + (rows - 1) * sa + ra) return false;
+  if (rows == 1 || (sa == ra && sb == rb)) return true;
+  if (sa != sb) return pa == pb;
+  const long long d = ((pb - pa) % sa + sa) % sa;                              // where b's rows begin between the beginnings of a's
+  return d < ra || sa - d < rb;
+}
+bool same_rows(const void* a, long long stride_a, const void* b, long long stride_b, long long rows) { return a == b && (rows <= 1 || stride_a == stride_b); }
+
 // The pointer is memory of the current device (a pointer of another one would be a fault on the GPU, not an error).
 rt_status on_current_device(const void* p) {
   int dev = 0;
@@ -100,6 +114,8 @@ rt_status rt_cache_read(const rt_paged_cache* cache, int32_t dtype, void* k, voi
   CacheRowsParams p;
   rt_status st = cache_rows(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, &p);
   if (st != RT_OK || rows == 0) return st;
+  const long long row = (long long)cache->n_kv_heads * cache->head_dim;
+  if (rows_overlap(k, dtype, k_stride, row, v, dtype, v_stride, row, rows)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   p.k_out = k; p.v_out = v;
   return cache_read_launch(dtype, p, (cudaStream_t)cuda_stream) == cudaSuccess ? RT_OK : RT_ERR_CUDA;
@@ -122,6 +138,10 @@ rt_status rt_paged_attention(const rt_paged_cache* cache, const rt_paged_query* 
   if (q->k_own && (!rows_ok(q->k_own, q->dtype, q->k_own_stride, kv_row, B) || !rows_ok(q->v_own, q->dtype, q->v_own_stride, kv_row, B)))
     return RT_ERR_INVALID_ARG;
   if (q->n_heads / cache->n_kv_heads > 1024 || !paged_attn_counts(cache, q->n_heads)) return RT_ERR_UNSUPPORTED;
+  if (rows_overlap(q->out, q->dtype, q->out_stride, row, q->q, q->dtype, q->q_stride, row, B) ||
+      (q->k_own && (rows_overlap(q->out, q->dtype, q->out_stride, row, q->k_own, q->dtype, q->k_own_stride, kv_row, B) ||
+                    rows_overlap(q->out, q->dtype, q->out_stride, row, q->v_own, q->dtype, q->v_own_stride, kv_row, B))))
+    return RT_ERR_INVALID_ARG;
   if (workspace_bytes < paged_attn_workspace(cache, q->n_heads)) return RT_ERR_WORKSPACE;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   PagedAttnParams p;
@@ -143,8 +163,13 @@ rt_status rt_qk_rotate(const rt_rotate_config* cfg, const void* q, const void* k
     return RT_ERR_INVALID_ARG;
   if (krow && (!rows_ok(k, cfg->dtype, k_stride, krow, rows) || !rows_ok(k_out, cfg->dtype, k_out_stride, krow, rows) || !aligned16(g_k)))
     return RT_ERR_INVALID_ARG;
-  if ((q == q_out && q_stride != q_out_stride && rows > 1) || (krow && k == k_out && k_stride != k_out_stride && rows > 1)) return RT_ERR_INVALID_ARG;
   if (rows == 0) return RT_OK;
+  const int t = cfg->dtype;
+  if (!same_rows(q, q_stride, q_out, q_out_stride, rows) && rows_overlap(q, t, q_stride, qrow, q_out, t, q_out_stride, qrow, rows)) return RT_ERR_INVALID_ARG;
+  if (krow && ((!same_rows(k, k_stride, k_out, k_out_stride, rows) && rows_overlap(k, t, k_stride, krow, k_out, t, k_out_stride, krow, rows)) ||
+               rows_overlap(q_out, t, q_out_stride, qrow, k_out, t, k_out_stride, krow, rows) || rows_overlap(q_out, t, q_out_stride, qrow, k, t, k_stride, krow, rows) ||
+               rows_overlap(k_out, t, k_out_stride, krow, q, t, q_stride, qrow, rows)))
+    return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(q)) != RT_OK) return st;
   RotateParams p;
   rotate_fill(cfg, &p);
@@ -169,6 +194,11 @@ rt_status rt_qk_rotate_backward(const rt_rotate_config* cfg, const void* q, cons
     return RT_ERR_INVALID_ARG;
   if (krow && (!rows_ok(k, cfg->dtype, k_stride, krow, rows) || !rows_ok(dk_out, RT_F32, krow, krow, rows) || !rows_ok(dk, RT_F32, krow, krow, rows) ||
                !aligned16(g_k) || !aligned16(dg_k)))
+    return RT_ERR_INVALID_ARG;
+  auto clash = [&](const void* a, long long ra, const void* b, long long rb) { return rows_overlap(a, RT_F32, ra, ra, b, RT_F32, rb, rb, rows); };
+  if ((dq != dq_out && clash(dq, qrow, dq_out, qrow)) || rows_overlap(dq, RT_F32, qrow, qrow, q, cfg->dtype, q_stride, qrow, rows)) return RT_ERR_INVALID_ARG;
+  if (krow && ((dk != dk_out && clash(dk, krow, dk_out, krow)) || clash(dq, qrow, dk, krow) || clash(dq, qrow, dk_out, krow) || clash(dk, krow, dq_out, qrow) ||
+               rows_overlap(dk, RT_F32, krow, krow, k, cfg->dtype, k_stride, krow, rows)))
     return RT_ERR_INVALID_ARG;
   if (workspace_bytes < rotate_backward_workspace(cfg->n_heads + cfg->n_kv_heads, cfg->head_dim, rows)) return RT_ERR_WORKSPACE;
   if ((st = on_current_device(workspace)) != RT_OK) return st;

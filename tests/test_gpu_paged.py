@@ -667,7 +667,7 @@ def test_tensors_that_are_refused():
     q = torch.zeros((2, 4, 64), device="cuda", dtype=torch.bfloat16)
     refused = [lambda: c.attend(q.cpu(), n), lambda: c.attend(q, n.cpu()), lambda: c.attend(q, n.long()), lambda: c.attend(q[:1], n), lambda: c.attend(q.half(), n),
                lambda: c.attend(q[:, :3], n), lambda: c.attend(q.transpose(1, 2).contiguous().transpose(1, 2), n), lambda: c.attend(q, n, k_own=q[:, :2]),
-               lambda: c.attend(q, n, out=torch.empty((2, 4, 64), device="cuda")), lambda: c.attend(q, n, lse=torch.empty((2, 4), device="cuda").double()),
+               lambda: c.attend(q, n, out=q), lambda: c.attend(q, n, out=torch.empty((2, 4, 64), device="cuda")), lambda: c.attend(q, n, lse=torch.empty((2, 4), device="cuda").double()),
                lambda: c.attend(q, n, alibi_slopes=torch.ones(3, device="cuda")), lambda: c.write(q[:, :2], q[:, :2], n, n[:1]),
                lambda: c.write(q, q, n, n), lambda: c.write(q[:, :2], q[:, :2].float(), n, n), lambda: c.read(n, n, k=torch.empty((2, 2, 64), device="cuda")),
                lambda: rt.PagedCache(c.k, c.v.transpose(2, 3), c.page_table), lambda: rt.PagedCache(c.k, c.v, c.page_table.long()),

@@ -18,7 +18,7 @@ def cache(**kw):
 
 
 def query(**kw):
-    q = rt.RtPagedQuery(ADDR, None, None, ADDR, None, ADDR, None, 128, 0, 0, 128, rt.RT_BF16, 2, 0.125)
+    q = rt.RtPagedQuery(ADDR, None, None, ADDR, None, ADDR + 4096, None, 128, 0, 0, 128, rt.RT_BF16, 2, 0.125)
     for n, x in kw.items():
         setattr(q, n, x)
     return q
@@ -55,7 +55,10 @@ def test_queries_that_are_refused():
     for kw in (dict(q=None), dict(out=None), dict(lens=None), dict(dtype=rt.RT_E4M3), dict(n_heads=0), dict(n_heads=3), dict(n_heads=-2), dict(k_own=ADDR),
                dict(v_own=ADDR), dict(k_own=ADDR, v_own=ADDR), dict(k_own=ADDR, v_own=ADDR, k_own_stride=128, v_own_stride=64), dict(q_stride=64),
                dict(q_stride=130), dict(out_stride=0), dict(q=ADDR + 2), dict(out=ADDR + 8), dict(lens=ADDR + 1), dict(alibi_slopes=ADDR + 2),
-               dict(lse=ADDR + 3), dict(softmax_scale=math.inf), dict(softmax_scale=math.nan), dict(ws=None), dict(ws=ADDR + 8)):
+               dict(lse=ADDR + 3), dict(softmax_scale=math.inf), dict(softmax_scale=math.nan), dict(ws=None), dict(ws=ADDR + 8),
+               # out on the queries, on their last row, on the own pairs
+               dict(out=ADDR), dict(out=ADDR + 512), dict(out=ADDR, out_stride=256),
+               dict(k_own=ADDR + 4096, v_own=ADDR, k_own_stride=128, v_own_stride=128)):
         assert call(**kw) == BAD, kw
     assert call(n_heads=2 * 2048, q_stride=2 * 2048 * 64, out_stride=2 * 2048 * 64) == UNSUPPORTED
     need = rt.rt_paged_attention_workspace_bytes(cache(), 2)
@@ -86,16 +89,17 @@ def test_rows_to_rotate_that_are_refused():
     base = dict(q=ADDR, k=ADDR + 256, qs=256, ks=128, gq=None, gk=None, pos=ADDR, rows=3, qo=ADDR, ko=ADDR + 256, qos=256, kos=128)
     call = lambda **kw: rt.rt_qk_rotate(config(), *{**base, **kw}.values(), None)
     for kw in (dict(q=None), dict(k=None), dict(pos=None), dict(rows=-1), dict(qo=None), dict(ko=None), dict(qs=128), dict(qs=260), dict(ks=100), dict(qos=0),
-               dict(kos=64), dict(gq=ADDR + 2), dict(gk=ADDR + 8), dict(q=ADDR + 8), dict(pos=ADDR + 2), dict(qos=264), dict(kos=136)):
+               dict(kos=64), dict(gq=ADDR + 2), dict(gk=ADDR + 8), dict(q=ADDR + 8), dict(pos=ADDR + 2), dict(qos=264), dict(kos=136), dict(qo=ADDR + 32), dict(qo=ADDR + 256), dict(ko=ADDR),
+               dict(qo=ADDR + 4096, ko=ADDR + 4096)):
         assert call(**kw) == BAD, kw
     assert call(rows=0) == rt.RT_OK
     need = rt.rt_qk_rotate_backward_workspace_bytes(config(), 1000)
     assert need >= rt.rt_qk_rotate_backward_workspace_bytes(config(), 10) >= rt.rt_qk_rotate_backward_workspace_bytes(config(), 0) > 0
     sizes = [rt.rt_qk_rotate_backward_workspace_bytes(config(), r) for r in (0, 1, 16, 17, 1000, 18943, 18944, 18945, 40000, 1 << 30)]
     assert sizes == sorted(sizes)                              # a workspace for many rows serves fewer
-    grad = dict(q=ADDR, k=ADDR, qs=256, ks=128, gq=None, gk=None, pos=ADDR, rows=1000, dqo=ADDR, dko=ADDR, dq=ADDR, dk=ADDR, dgq=None, dgk=None, ws=ADDR, n=need)
+    grad = dict(q=ADDR, k=ADDR, qs=256, ks=128, gq=None, gk=None, pos=ADDR, rows=1000, dqo=ADDR, dko=ADDR + (1 << 24), dq=ADDR + (1 << 25), dk=ADDR + (1 << 26), dgq=None, dgk=None, ws=ADDR, n=need)
     call = lambda **kw: rt.rt_qk_rotate_backward(config(), *{**grad, **kw}.values(), None)
     for kw in (dict(q=None), dict(dqo=None), dict(dko=None), dict(dq=None), dict(dk=None), dict(dqo=ADDR + 4), dict(dk=ADDR + 8), dict(dgq=ADDR + 4), dict(ws=None),
-               dict(ws=ADDR + 16 + 4), dict(rows=-1), dict(qs=0)):
+               dict(ws=ADDR + 16 + 4), dict(rows=-1), dict(qs=0), dict(dq=ADDR + 16), dict(dk=ADDR), dict(dq=ADDR + (1 << 24)), dict(dk=ADDR + (1 << 25))):
         assert call(**kw) == BAD, kw
     assert call(n=need - 1) == rt.RT_ERR_WORKSPACE
