@@ -710,6 +710,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<CT, HD>::CTAS) paged_attn_k
     unsigned rest = u0 - sums[lo];
     int b = lo * ln.per;
     for (;; ++b) {
+      if (b >= p.c.n_seqs) return;                                             // (only if somebody changes the lengths meanwhile)
       cc.n = clamp_len(p, b);
       cc.tiles = tiles_of<S::KT>(cc.n);
       const unsigned here = (unsigned)cc.tiles * items;
@@ -893,7 +894,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __gri
     for (int s = b / ln.per * ln.per; s < b; ++s) u += (unsigned)tiles_of<KT>(clamp_len(p, s)) * items;
     const int tiles = tiles_of<KT>(n), g = h % p.group;
     u += (unsigned)(h / p.group * slices + g / kRows) * tiles;
-    const unsigned w0 = ln.worker_of(u), w1 = ln.worker_of(u + tiles - 1);
+    const unsigned w0 = min(ln.worker_of(u), ln.workers - 1), w1 = min(ln.worker_of(u + tiles - 1), ln.workers - 1);      // (min: as above)
     if (w0 == w1) continue;                                            // written by the warp that held all of it
     const int r = g % kRows;
     Own<HD> own;
