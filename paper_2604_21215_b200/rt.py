@@ -298,14 +298,18 @@ def make_config(d_model: int, n_heads: int, d_ff: int, dtype: str = "bf16", sche
 
 # ------------------------------------------------------------------ conveniences on torch tensors
 
-_torch_module = None
+_torch_module = _device_now = _stream_now = None
 
 
 def _torch():
-    global _torch_module
+    global _torch_module, _device_now, _stream_now
     if _torch_module is None:
         import torch
         _torch_module = torch
+        # the current device, and a device's current stream as a number (torch.cuda.current_stream builds an object for it, 2 us);
+        # a torch without CUDA has neither, and the calls that need them refuse its arrays
+        _device_now = getattr(torch._C, "_cuda_getDevice", lambda: -1)
+        _stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return _torch_module
 
 
@@ -325,10 +329,6 @@ def _require(ok: bool, where: str):
     """What ctypes cannot see of a tensor (its device, type, shape, the order of its dimensions) is refused like a bad argument of the call."""
     if not ok:
         raise RtError(RT_ERR_INVALID_ARG, where)
-
-
-def _on_device(torch, index: int) -> bool:
-    return torch._C._cuda_getDevice() == index
 
 
 def _rows(t, heads: int, head_dim: int, n: int, dtype, index: int, where: str) -> tuple:
@@ -616,6 +616,7 @@ class PagedCache:
                                self._status.data_ptr(), n_pages, page, n_kv, hd, code, page_table.shape[0], page_table.shape[1])
         self._index = k.device.index
         self._ref, self._scale = C.byref(self._c), 1.0 / math.sqrt(hd)
+        self._B, self._kv, self._hd = page_table.shape[0], n_kv, hd
         self._codes = {torch.float32: RT_F32, torch.bfloat16: RT_BF16}
         self._ws_like: dict = {}                       # by number of query heads: one word seen as an array of the workspace's size
         _require(rt_paged_attention_workspace_bytes(self._c, n_kv) > 0, "PagedCache: shape")
@@ -631,31 +632,32 @@ class PagedCache:
         exps = lambda: torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype == "e4m3" else None
         return cls(pool(), pool(), torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), exps(), exps())
 
-    # (The methods below are called for every layer and token: checks and arguments are kept to the few microseconds that they need.  Arrays made here
-    # need no check, and torch._C gives the current stream as a number, where torch.cuda.current_stream builds an object for it.)
+    # (The methods below are called for every layer and token: checks and arguments are kept to the few microseconds that they need.)
 
     def write(self, k, v, seq, pos) -> None:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
         seq[r] (int32); a negative position skips the row."""
-        torch, c, dev, n, t = _torch(), self._c, self._index, k.shape[0], k.dtype
-        if not _on_device(torch, dev):
+        torch, kv, hd, dev, n, t = _torch(), self._kv, self._hd, self._index, k.shape[0], k.dtype
+        if _device_now() != dev:
             with torch.cuda.device(dev):
                 return self.write(k, v, seq, pos)
         code = self._codes.get(t)
         _require(code is not None, "PagedCache.write: k")
-        kp, ks = _rows(k, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.write: k")
-        vp, vs = _rows(v, c.n_kv_heads, c.head_dim, n, t, dev, "PagedCache.write: v")
+        kp, ks = _rows(k, kv, hd, n, t, dev, "PagedCache.write: k")
+        vp, vs = _rows(v, kv, hd, n, t, dev, "PagedCache.write: v")
         sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.write: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.write: pos")
-        _check(_lib.rt_cache_write(self._ref, code, kp, vp, ks, vs, sp, pp, n, torch._C._cuda_getCurrentRawStream(dev)), "rt_cache_write")
+        status = _lib.rt_cache_write(self._ref, code, kp, vp, ks, vs, sp, pp, n, _stream_now(dev))
+        if status:
+            raise RtError(status, "rt_cache_write")
 
     def read(self, seq, pos, dtype: str = "bf16", k=None, v=None):
         """Rows (seq[r], pos[r]) as `dtype` ("f32", "bf16") -> k, v [rows, n_kv_heads, head_dim]; into k and v where they are given.
         Rows that are skipped stay as they are (in arrays made here: whatever the memory holds)."""
-        torch, c, dev, n = _torch(), self._c, self._index, pos.shape[0]
-        if not _on_device(torch, dev):
+        torch, kv, hd, dev, n = _torch(), self._kv, self._hd, self._index, pos.shape[0]
+        if _device_now() != dev:
             with torch.cuda.device(dev):
                 return self.read(seq, pos, dtype, k, v)
-        kv, hd, t = c.n_kv_heads, c.head_dim, torch.bfloat16 if dtype == "bf16" else _tdtype(dtype)
+        t = torch.bfloat16 if dtype == "bf16" else _tdtype(dtype)
         ks = vs = kv * hd
         if k is None:
             k = self.k.new_empty((n, kv, hd), dtype=t)
@@ -668,7 +670,9 @@ class PagedCache:
         else:
             vp, vs = _rows(v, kv, hd, n, t, dev, "PagedCache.read: v")
         sp, pp = _vector(seq, n, torch.int32, dev, "PagedCache.read: seq"), _vector(pos, n, torch.int32, dev, "PagedCache.read: pos")
-        _check(_lib.rt_cache_read(self._ref, self._codes[t], kp, vp, ks, vs, sp, pp, n, torch._C._cuda_getCurrentRawStream(dev)), "rt_cache_read")
+        status = _lib.rt_cache_read(self._ref, self._codes[t], kp, vp, ks, vs, sp, pp, n, _stream_now(dev))
+        if status:
+            raise RtError(status, "rt_cache_read")
         return k, v
 
     def attend(self, q, lens, k_own=None, v_own=None, scale: Optional[float] = None, alibi_slopes=None, out=None, lse=None):
@@ -676,11 +680,10 @@ class PagedCache:
         if given, to its own pair k_own, v_own [n_seqs, n_kv_heads, head_dim] -> out [n_seqs, n_heads, head_dim].  lse (float32
         [n_seqs, n_heads]) is filled if given; a sequence of negative length keeps its rows of out and lse (a new out:
         whatever the memory holds)."""
-        torch, c, dev = _torch(), self._c, self._index
-        if not _on_device(torch, dev):
+        torch, B, kv, hd, dev, t = _torch(), self._B, self._kv, self._hd, self._index, q.dtype
+        if _device_now() != dev:
             with torch.cuda.device(dev):
                 return self.attend(q, lens, k_own, v_own, scale, alibi_slopes, out, lse)
-        B, kv, hd, t = c.n_seqs, c.n_kv_heads, c.head_dim, q.dtype
         code = self._codes.get(t)
         _require(code is not None and q.dim() == 3, "PagedCache.attend: q")
         H = q.shape[1]
@@ -703,13 +706,14 @@ class PagedCache:
         a.dtype, a.n_heads, a.softmax_scale = code, H, self._scale if scale is None else scale
         like = self._ws_like.get(H)
         if like is None:
-            need = rt_paged_attention_workspace_bytes(c, H)
+            need = rt_paged_attention_workspace_bytes(self._c, H)
             _require(need > 0, "PagedCache.attend: q")
             like = self._ws_like[H] = self._status.expand(need // 4)
         # a workspace of its own for every call: calls on two streams, or two captured graphs, may overlap
         ws = torch.empty_like(like, memory_format=torch.contiguous_format)
-        _check(_lib.rt_paged_attention(self._ref, C.byref(a), ws.data_ptr(), 4 * like.shape[0], torch._C._cuda_getCurrentRawStream(dev)),
-               "rt_paged_attention")
+        status = _lib.rt_paged_attention(self._ref, C.byref(a), ws.data_ptr(), 4 * like.shape[0], _stream_now(dev))
+        if status:
+            raise RtError(status, "rt_paged_attention")
         return out
 
     def status(self) -> int:
@@ -751,7 +755,7 @@ class QkRotate:
         """q [rows, n_heads, head_dim], k [rows, n_kv_heads, head_dim] at any row stride, pos [rows] int32 -> q_out, k_out (which may be q
         and k).  Rows of negative position stay as they are (in arrays made here: whatever the memory holds)."""
         torch, H, kv, hd = _torch(), self.n_heads, self.n_kv_heads, self.head_dim
-        if q.is_cuda and not _on_device(torch, q.get_device()):
+        if q.is_cuda and _device_now() != q.get_device():
             with torch.cuda.device(q.get_device()):
                 return self.forward(q, k, pos, g_q, g_k, q_out, k_out)
         n, t, dev, qp, qs, kp, ks, gq, gk, pp = self._inputs(q, k, pos, g_q, g_k)
@@ -766,14 +770,16 @@ class QkRotate:
             ko = k_out.data_ptr()
         elif kv:
             ko, kos = _rows(k_out, kv, hd, n, t, dev, "QkRotate.forward: k_out")
-        _check(_lib.rt_qk_rotate(self._ref, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, torch._C._cuda_getCurrentRawStream(dev)), "rt_qk_rotate")
+        status = _lib.rt_qk_rotate(self._ref, qp, kp, qs, ks, gq, gk, pp, n, qo, ko, qos, kos, _stream_now(dev))
+        if status:
+            raise RtError(status, "rt_qk_rotate")
         return q_out, k_out
 
     def backward(self, q, k, pos, dq_out, dk_out, g_q=None, g_k=None, dq=None, dk=None):
         """The inputs of forward and the gradients of its outputs (float32, contiguous) -> dq, dk, dg_q, dg_k (float32; dg is None where the
         gain is).  dq and dk may be given, dq_out and dk_out themselves among them; rows of negative position stay as they are."""
         torch, H, kv, hd = _torch(), self.n_heads, self.n_kv_heads, self.head_dim
-        if q.is_cuda and not _on_device(torch, q.get_device()):
+        if q.is_cuda and _device_now() != q.get_device():
             with torch.cuda.device(q.get_device()):
                 return self.backward(q, k, pos, dq_out, dk_out, g_q, g_k, dq, dk)
         f32 = torch.float32
@@ -794,10 +800,12 @@ class QkRotate:
                 dkp = _vector(dk, n * kv * hd, f32, dev, "QkRotate.backward: dk")
             dgk = None if gk is None else torch.empty_like(g_k, dtype=f32)
         dgq = None if gq is None else torch.empty_like(g_q, dtype=f32)
-        if self._need[0] != n:
-            self._need = (n, rt_qk_rotate_backward_workspace_bytes(self.cfg, n))
-        ws = dq_out.new_empty(self._need[1] // 4)
-        _check(_lib.rt_qk_rotate_backward(self._ref, qp, kp, qs, ks, gq, gk, pp, n, dqo, dko, dqp, dkp, None if dgq is None else dgq.data_ptr(),
-                                          None if dgk is None else dgk.data_ptr(), ws.data_ptr(), self._need[1],
-                                          torch._C._cuda_getCurrentRawStream(dev)), "rt_qk_rotate_backward")
+        need = self._need
+        if need[0] != n:
+            need = self._need = (n, rt_qk_rotate_backward_workspace_bytes(self.cfg, n))
+        ws = dq_out.new_empty(need[1] // 4)
+        status = _lib.rt_qk_rotate_backward(self._ref, qp, kp, qs, ks, gq, gk, pp, n, dqo, dko, dqp, dkp, None if dgq is None else dgq.data_ptr(),
+                                            None if dgk is None else dgk.data_ptr(), ws.data_ptr(), need[1], _stream_now(dev))
+        if status:
+            raise RtError(status, "rt_qk_rotate_backward")
         return dq, dk, dgq, dgk
