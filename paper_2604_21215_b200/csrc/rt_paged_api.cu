@@ -50,6 +50,26 @@ bool rows_overlap(const void* a, int dtype_a, long long stride_a, long long row_
   const long long d = ((pb - pa) % sa + sa) % sa;                              // where b's rows begin between the beginnings of a's
   return d < ra || sa - d < rb;
 }
+// Whether the bytes of an array lie in a cache's pools, or the pools in one another.
+bool ranges_overlap(const void* a, long long na, const void* b, long long nb) {
+  const intptr_t pa = reinterpret_cast<intptr_t>(a), pb = reinterpret_cast<intptr_t>(b);
+  return a && b && pa < pb + nb && pb < pa + na;
+}
+struct Pools {
+  const void* at[4];
+  long long bytes[4];
+  explicit Pools(const rt_paged_cache* c) : at{c->k, c->v, c->k_exp, c->v_exp} {
+    const long long heads_rows = (long long)c->n_pages * c->n_kv_heads * c->page_size;
+    bytes[0] = bytes[1] = heads_rows * c->head_dim * (c->dtype == RT_E4M3 ? 1 : esize(c->dtype));
+    bytes[2] = bytes[3] = heads_rows;
+  }
+  bool meet(const void* p, long long n, int first = 0) const {
+    for (int i = first; i < 4; ++i) if (ranges_overlap(p, n, at[i], bytes[i])) return true;
+    return false;
+  }
+  bool meet_each_other() const { return meet(at[0], bytes[0], 1) || meet(at[1], bytes[1], 2) || meet(at[2], bytes[2], 3); }
+};
+long long extent(int dtype, long long stride, long long row, long long rows) { return ((rows - 1) * (rows > 1 ? stride : 0) + row) * esize(dtype); }
 bool same_rows(const void* a, long long stride_a, const void* b, long long stride_b, long long rows) { return a == b && (rows <= 1 || stride_a == stride_b); }
 
 // The pointer is memory of the current device (a pointer of another one would be a fault on the GPU, not an error).
@@ -104,6 +124,9 @@ rt_status rt_cache_write(const rt_paged_cache* cache, int32_t dtype, const void*
   CacheRowsParams p;
   rt_status st = cache_rows(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, &p);
   if (st != RT_OK || rows == 0) return st;
+  const long long row = (long long)cache->n_kv_heads * cache->head_dim;
+  const Pools pools(cache);
+  if (pools.meet_each_other() || pools.meet(k, extent(dtype, k_stride, row, rows)) || pools.meet(v, extent(dtype, v_stride, row, rows))) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   p.k_in = k; p.v_in = v;
   return cache_write_launch(dtype, p, (cudaStream_t)cuda_stream) == cudaSuccess ? RT_OK : RT_ERR_CUDA;
@@ -115,7 +138,10 @@ rt_status rt_cache_read(const rt_paged_cache* cache, int32_t dtype, void* k, voi
   rt_status st = cache_rows(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, &p);
   if (st != RT_OK || rows == 0) return st;
   const long long row = (long long)cache->n_kv_heads * cache->head_dim;
-  if (rows_overlap(k, dtype, k_stride, row, v, dtype, v_stride, row, rows)) return RT_ERR_INVALID_ARG;
+  const Pools pools(cache);
+  if (rows_overlap(k, dtype, k_stride, row, v, dtype, v_stride, row, rows) || pools.meet(k, extent(dtype, k_stride, row, rows)) ||
+      pools.meet(v, extent(dtype, v_stride, row, rows)))
+    return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   p.k_out = k; p.v_out = v;
   return cache_read_launch(dtype, p, (cudaStream_t)cuda_stream) == cudaSuccess ? RT_OK : RT_ERR_CUDA;
@@ -143,6 +169,8 @@ rt_status rt_paged_attention(const rt_paged_cache* cache, const rt_paged_query* 
                     rows_overlap(q->out, q->dtype, q->out_stride, row, q->v_own, q->dtype, q->v_own_stride, kv_row, B))))
     return RT_ERR_INVALID_ARG;
   if (workspace_bytes < paged_attn_workspace(cache, q->n_heads)) return RT_ERR_WORKSPACE;
+  const Pools pools(cache);
+  if (pools.meet(q->out, extent(q->dtype, q->out_stride, row, B)) || pools.meet(q->lse, 4 * B * q->n_heads)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   PagedAttnParams p;
   memset(&p, 0, sizeof(p));
@@ -198,7 +226,8 @@ rt_status rt_qk_rotate_backward(const rt_rotate_config* cfg, const void* q, cons
   auto clash = [&](const void* a, long long ra, const void* b, long long rb) { return rows_overlap(a, RT_F32, ra, ra, b, RT_F32, rb, rb, rows); };
   if ((dq != dq_out && clash(dq, qrow, dq_out, qrow)) || rows_overlap(dq, RT_F32, qrow, qrow, q, cfg->dtype, q_stride, qrow, rows)) return RT_ERR_INVALID_ARG;
   if (krow && ((dk != dk_out && clash(dk, krow, dk_out, krow)) || clash(dq, qrow, dk, krow) || clash(dq, qrow, dk_out, krow) || clash(dk, krow, dq_out, qrow) ||
-               rows_overlap(dk, RT_F32, krow, krow, k, cfg->dtype, k_stride, krow, rows)))
+               rows_overlap(dk, RT_F32, krow, krow, k, cfg->dtype, k_stride, krow, rows) || rows_overlap(dq, RT_F32, qrow, qrow, k, cfg->dtype, k_stride, krow, rows) ||
+               rows_overlap(dk, RT_F32, krow, krow, q, cfg->dtype, q_stride, qrow, rows) || ranges_overlap(dg_q, 4 * qrow, dg_k, 4 * krow)))
     return RT_ERR_INVALID_ARG;
   if (workspace_bytes < rotate_backward_workspace(cfg->n_heads + cfg->n_kv_heads, cfg->head_dim, rows)) return RT_ERR_WORKSPACE;
   if ((st = on_current_device(workspace)) != RT_OK) return st;

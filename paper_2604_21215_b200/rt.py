@@ -636,7 +636,7 @@ class PagedCache:
 
     def write(self, k, v, seq, pos) -> None:
         """Row r of k and v ([rows, n_kv_heads, head_dim], float32 or bfloat16, rows at any stride) becomes position pos[r] of sequence
-        seq[r] (int32); a negative position skips the row."""
+        seq[r] (int32); a negative position skips the row.  The rows of a call name different places."""
         torch, kv, hd, dev, n, t = _torch(), self._kv, self._hd, self._index, k.shape[0], k.dtype
         if _device_now() != dev:
             with torch.cuda.device(dev):

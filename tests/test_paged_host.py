@@ -103,3 +103,23 @@ def test_rows_to_rotate_that_are_refused():
                dict(ws=ADDR + 16 + 4), dict(rows=-1), dict(qs=0), dict(dq=ADDR + 16), dict(dk=ADDR), dict(dq=ADDR + (1 << 24)), dict(dk=ADDR + (1 << 25))):
         assert call(**kw) == BAD, kw
     assert call(n=need - 1) == rt.RT_ERR_WORKSPACE
+
+
+def test_outputs_that_lie_in_the_pools_or_on_inputs_of_the_other_kind():
+    big = 1 << 24
+    apart = lambda **kw: cache(**{**dict(v=ADDR + big), **kw})                # pools of 32 KB
+    write = lambda c, k, v: rt.rt_cache_write(c, rt.RT_BF16, k, v, 128, 128, ADDR, ADDR, 4, None)
+    read = lambda c, k, v: rt.rt_cache_read(c, rt.RT_BF16, k, v, 128, 128, ADDR, ADDR, 4, None)
+    assert write(cache(), ADDR + 2 * big, ADDR + 3 * big) == BAD             # keys and values in one pool
+    for f in (write, read):
+        assert f(apart(), ADDR + 16, ADDR + 3 * big) == BAD and f(apart(), ADDR + 3 * big, ADDR + big + 32768 - 16) == BAD
+        assert f(apart(), ADDR + big - 512, ADDR + 3 * big) == BAD             # the last row reaches the values' first
+    f8 = apart(dtype=rt.RT_E4M3, k_exp=ADDR + 4 * big, v_exp=ADDR + 5 * big)
+    assert write(f8, ADDR + 5 * big, ADDR + 3 * big) == BAD and write(apart(dtype=rt.RT_E4M3, k_exp=ADDR + 4 * big, v_exp=ADDR + 4 * big), ADDR + 2 * big, ADDR + 3 * big) == BAD
+    attend = lambda **kw: rt.rt_paged_attention(apart(), query(**{**dict(q=ADDR + 2 * big, out=ADDR + 3 * big), **kw}), ADDR, 1 << 40, None)
+    assert attend(out=ADDR + 4096) == BAD and attend(out=ADDR + big - 16) == BAD and attend(lse=ADDR + big + 32764) == BAD
+    grad = dict(q=ADDR, k=ADDR + big, qs=256, ks=128, gq=None, gk=None, pos=ADDR, rows=100, dqo=ADDR + 2 * big, dko=ADDR + 3 * big, dq=ADDR + 4 * big, dk=ADDR + 5 * big,
+                dgq=None, dgk=None, ws=ADDR, n=1 << 40)
+    call = lambda **kw: rt.rt_qk_rotate_backward(config(), *{**grad, **kw}.values(), None)
+    for kw in (dict(dq=ADDR + big), dict(dk=ADDR), dict(dgq=ADDR + 6 * big, dgk=ADDR + 6 * big), dict(dgq=ADDR + 6 * big, dgk=ADDR + 6 * big + 256)):
+        assert call(**kw) == BAD, kw
