@@ -329,7 +329,7 @@ rt_status rt_paged_attention(const rt_paged_cache *cache, const rt_paged_query *
  *   y = x / sqrt(mean(x^2) + rms_eps) * g          (with norm_flags = RT_NORM_QK; otherwise y = x)
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),   t = pos[r] * freq[i],  i < rot_dim / 2
  * with (a, b) = (i, i + rot_dim / 2) for RT_PAIRS_HALVES and (2 i, 2 i + 1) for RT_PAIRS_NEIGHBOURS; dimensions from rot_dim on are
- * not rotated.  Angles are formed in 64 bits.  q_out may be q and k_out may be k (with the same stride). */
+ * not rotated.  Turns are multiplied in 64 bits; sine and cosine are fp32's, with RT_BF16 to 2^-21.  q_out may be q and k_out may be k (with the same stride). */
 enum { RT_PAIRS_HALVES = 0, RT_PAIRS_NEIGHBOURS = 1 };
 typedef struct {
   int32_t dtype;                   /* RT_F32 or RT_BF16: queries, keys, gains and their outputs */

@@ -40,7 +40,7 @@ struct RotateParams {
   int rows;
   const float *dq_out, *dk_out;       // backward
   float *dq, *dk, *dg_q, *dg_k;
-  double turns[kMaxRot / 2];          // freq / (2 pi): full turns per position
+  unsigned long long turns[kMaxRot / 2];      // turns per position, whole ones left out, in 2^-64 turns
 };
 cudaError_t rotate_launch(int dtype, const RotateParams& p, cudaStream_t s);
 cudaError_t rotate_backward_launch(int dtype, const RotateParams& p, void* workspace, cudaStream_t s);

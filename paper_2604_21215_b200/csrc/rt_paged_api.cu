@@ -112,7 +112,12 @@ void rotate_fill(const rt_rotate_config* c, RotateParams* p) {
   p->n_heads = c->n_heads; p->n_kv = c->n_kv_heads; p->hd = c->head_dim;
   p->norm = (c->norm_flags & RT_NORM_QK) != 0; p->rot = c->rot_dim; p->neighbours = c->pairs == RT_PAIRS_NEIGHBOURS;
   p->eps = c->rms_eps;
-  for (int i = 0; i < c->rot_dim / 2; ++i) p->turns[i] = c->freq[i] / 6.283185307179586476925286766559;
+  for (int i = 0; i < c->rot_dim / 2; ++i) {
+    double t = c->freq[i] / 6.283185307179586476925286766559;
+    t -= rint(t);                                                             // (exact)
+    const unsigned long long n = (unsigned long long)ldexp(fabs(t), 64);      // at most 2^63
+    p->turns[i] = t < 0 ? 0 - n : n;
+  }
 }
 
 }  // namespace

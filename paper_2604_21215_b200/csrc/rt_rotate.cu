@@ -1,12 +1,13 @@
 // qkRMS of queries and keys for each head and the rotation by the position, in one pass, and its backward pass.
 //
-// Bound: HBM traffic.  head_dim / 8 neighbouring lanes hold a row of a head; each holds the two sides a[i], b[i] of four pairs of dimensions, as
+// Bound: HBM traffic, if the instructions are few.  head_dim / 8 neighbouring lanes hold a row of a head; each holds the two sides a[i], b[i] of four pairs of dimensions, as
 // two loads of 4 elements, so the rotation needs no exchange and the norm a few shuffles.  Dimensions that are not rotated make pairs too, with an angle
-// of zero.  A warp takes the heads of one row side by side and one after the other: its lanes form the row's angles once, one or two each.  All products are paired fp32
-// instructions: at 6.5 TB/s an SM has 1370 issue slots for a row of 16 + 16 heads in bf16, and the pass takes 930.
-// Measured on one B200, of 6.55 TB/s: 8 x 4000 rows of 16 + 16 heads of 64 with gains, bf16 50 us (81 %), fp32 90 %; gradients 111 us (92 %).  Heads of 128, whose rows carry twice the
-// angles for as many bytes, 65 and 62 %; 16 query and 4 key heads 53 and 67 %.
+// of zero.  A warp takes the heads of one row side by side: its lanes form the row's angles once, one or two each.  All products are paired fp32
+// instructions.
+// Measured on one B200, of 6.55 TB/s: 8 x 4050 rows of 16 + 16 heads of 64 with gains, bf16 44 us (92 %), fp32 89 %; 8 + 8 heads of 128 93 %, 16 + 4 of 64 89 %, 16 + 4 of 128 84 %,
+// 4 + 4 of 64 57 % in bf16 (angles and addresses of a short row), 100 % in fp32.  Gradients 111 us (91 %), heads of 128 64 %.
 #include "rt_paged.h"
+#include "rt_tc.cuh"
 
 namespace rt {
 namespace {
@@ -34,11 +35,13 @@ template <typename T> struct Run;
 template <> struct Run<float> {
   float4 v;
   __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void ones() { v = make_float4(1.f, 1.f, 1.f, 1.f); }
   __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
 };
 template <> struct Run<__nv_bfloat16> {
   uint2 v;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void ones() { v = make_uint2(0x3f803f80u, 0x3f803f80u); }
   __device__ __forceinline__ void get(float (&f)[4]) const {
     f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
     f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
@@ -47,10 +50,40 @@ template <> struct Run<__nv_bfloat16> {
 __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = make_uint2(pack2(a, b), pack2(c, d)); }
 
+// asynchronous copies of one run, or one position, of a lane's own
+template <int BYTES>
+__device__ __forceinline__ void copy_run(unsigned to, const void* from) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A warp's ring of passes in shared memory: a pass is AHEAD places of two runs for each lane, and one position.  Every lane reads what it copied itself, so no lane
+// waits for another's, and nothing but the copies' completion is waited for.
+template <typename T, int AHEAD, int STAGES> struct Ring {
+  static constexpr int RUN = 4 * (int)sizeof(T), PASS = 32 * (AHEAD * 2 * RUN + 4), WARP = STAGES * PASS, BLOCK = kThreads / 32 * WARP;
+  unsigned char* mine;
+  unsigned at;
+  int lane;
+  __device__ __forceinline__ Ring(unsigned char* smem, int warp, int lane_) : mine(smem + warp * WARP), at((unsigned)__cvta_generic_to_shared(mine)), lane(lane_) {}
+  __device__ __forceinline__ void copy(int stage, int u, const T* x, const T* y) const {
+    copy_run<RUN>(at + stage * PASS + ((2 * u) * 32 + lane) * RUN, x);
+    copy_run<RUN>(at + stage * PASS + ((2 * u + 1) * 32 + lane) * RUN, y);
+  }
+  __device__ __forceinline__ void copy_pos(int stage, const int* pos) const { copy_run<4>(at + stage * PASS + 64 * AHEAD * RUN + 4 * lane, pos); }
+  __device__ __forceinline__ int& pos(int stage) const { return reinterpret_cast<int*>(mine + stage * PASS + 64 * AHEAD * RUN)[lane]; }
+  template <typename R> __device__ __forceinline__ void get(int stage, int u, R& r) const {
+    r.x.load(reinterpret_cast<const T*>(mine + stage * PASS + ((2 * u) * 32 + lane) * RUN));
+    r.y.load(reinterpret_cast<const T*>(mine + stage * PASS + ((2 * u + 1) * 32 + lane) * RUN));
+  }
+};
+
 // the two runs of a lane, and its pairs' sides: a[0] = sides a of pairs 0 and 1, a[1] of 2 and 3, b likewise
 template <typename T> struct Runs {
   Run<T> x, y;
   __device__ __forceinline__ void load(const T* row, const Lane& l) { x.load(row + l.first); y.load(row + l.second); }
+  __device__ __forceinline__ void ones() { x.ones(); y.ones(); }
 };
 struct Pairs { F2 a[2], b[2]; };
 template <bool NEIGHBOURS, typename T>
@@ -104,119 +137,158 @@ struct Turn {
 };
 
 // Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair through 512 bytes of shared memory of the warp's own (two loads a lane,
-// where shuffles would be 8 or 16); the turns are reduced in 64 bits, so that far positions keep their angles.  All lanes of the warp call.
+// where shuffles would be 8 or 16).  Turns are multiplied as 64-bit fractions, whole turns falling off at the top: far positions keep their angles (2^-34 turns from
+// the rounding of a turn, 2^-33 from that of the product to 32 bits, 2^-24 of itself in fp32), and it takes two integer products where fp64 would take six slow instructions.
 struct Angles { float cos[64], sin[64]; };
-template <int LPR>
-__device__ __forceinline__ Turn angles(const RotateParams& p, int pos, int lane, Angles& buf) {
-  __syncwarp();                                                        // (what was there is read)
+template <int LPR> struct Turns {                                      // of this lane's pairs
+  unsigned long long per[LPR / 8];
+  __device__ __forceinline__ Turns(const RotateParams& p, int lane) {
 #pragma unroll
-  for (int k = 0; k < LPR / 8; ++k) {
-    float co = 1.f, si = 0.f;
-    const int n = lane + 32 * k;
-    if (2 * n < p.rot) {
-      const double t = (double)pos * p.turns[n];
-      sincospif((float)(2.0 * (t - rint(t))), &si, &co);
-    }
-    buf.cos[n] = co;
-    buf.sin[n] = si;
+    for (int k = 0; k < LPR / 8; ++k) per[k] = p.turns[lane + 32 * k];      // (zero where there is no pair)
   }
-  __syncwarp();
-  const float4 c = reinterpret_cast<const float4*>(buf.cos)[lane % LPR], s = reinterpret_cast<const float4*>(buf.sin)[lane % LPR];
-  return {{f2(c.x, c.y), f2(c.z, c.w)}, {f2(s.x, s.y), f2(s.z, s.w)}, {f2(-s.x, -s.y), f2(-s.z, -s.w)}};
-}
+  // EXACT: to fp32's rounding; otherwise to 2^-21, for rows that are rounded to bf16 (2^-9)
+  template <bool EXACT>
+  __device__ __forceinline__ void make(int pos, int lane, Angles& buf) const {
+#pragma unroll
+    for (int k = 0; k < LPR / 8; ++k) {
+      const int half_turns = (int)((per[k] * (unsigned)pos + 0x80000000u) >> 32);      // in 2^-31
+      float co, si;
+      if (EXACT) sincospif((float)half_turns * 4.656612873077392578125e-10f, &si, &co);
+      else __sincosf((float)half_turns * (4.656612873077392578125e-10f * 3.14159265358979f), &si, &co);
+      buf.cos[lane + 32 * k] = co;
+      buf.sin[lane + 32 * k] = si;
+    }
+  }
+  __device__ __forceinline__ static Turn of(const Angles& buf, int lane) {
+    const float4 c = reinterpret_cast<const float4*>(buf.cos)[lane % LPR], s = reinterpret_cast<const float4*>(buf.sin)[lane % LPR];
+    return {{f2(c.x, c.y), f2(c.z, c.w)}, {f2(s.x, s.y), f2(s.z, s.w)}, {f2(-s.x, -s.y), f2(-s.z, -s.w)}};
+  }
+  // one row's, all lanes of the warp together
+  template <bool EXACT>
+  __device__ __forceinline__ Turn at(int pos, int lane, Angles& buf) const {
+    __syncwarp();                                                      // (what was there is read)
+    make<EXACT>(pos, lane, buf);
+    __syncwarp();
+    return of(buf, lane);
+  }
+};
 
-// The heads of a launch in block rows of the grid: heads_per of the queries' heads each in the first y_q of them, then heads_per of the keys' heads each.  All heads
-// in one block row where there are rows enough to fill the GPU, some of them in small calls, where a warp's chain of heads would be the call's time.
-struct Part { bool is_q; int first, last; };
-__device__ __forceinline__ Part part_of(const RotateParams& p, int y, int heads_per, int y_q) {
-  const bool is_q = y < y_q;
-  const int first = (is_q ? y : y - y_q) * heads_per;
-  return {is_q, first, min(is_q ? p.n_heads : p.n_kv, first + heads_per)};
-}
-
-constexpr int kBlocks = 3;      // of an SM, by registers
-// AHEAD: heads of a lane in flight, and as many on their way.  WHOLE: every block row's heads fill whole batches of them (otherwise lanes without a head
-// repeat the last one's, for the shuffles).
-template <typename T, int LPR, bool NEIGHBOURS, int AHEAD, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateParams p, int heads_per, int y_q) {
-  constexpr int HPW = 32 / LPR, HD = LPR * 8, BATCH = HPW * AHEAD;
-  __shared__ __align__(16) Angles bufs[kThreads / 32];
-  Angles& buf = bufs[threadIdx.x >> 5];
-  const int lane = threadIdx.x & 31, hl = lane / LPR;
+// Forward.  The heads of a row, queries' first, then keys', are a line; a warp has AHEAD * 32 / LPR places and goes from row to row.
+//   kOneKind: block row y of the grid takes the y-th part of the line, all queries or all keys, and no place is empty (one address and constants)
+//   kMixed: the same, whatever the parts hold
+//   kSideBySide: the line takes half of the places or less, and rows_per rows lie in them side by side, so that no lane idles and a pass moves bytes enough
+// Either way a pass is all that the warp does for its row: its gains stay in registers, its angles are formed once.
+enum Places { kOneKind, kMixed, kSideBySide };
+template <typename T, Places PLACES> constexpr int kMost = sizeof(T) == 2 && PLACES == kMixed ? 5 : 4;      // places of a lane, by registers
+constexpr int kSide = 4;                                                                                     // rows side by side
+// Blocks of an SM, and passes of a warp's ring.  Sixteen warps with one pass on its way each are faster than 24, or than two passes (16 + 16 heads of 64, bf16, two
+// passes a row: 45.7 us; 24 warps 46.4, 32 47.0; with two on their way 45.9, 49, 55; with the pass in registers instead of the ring 51).  Small passes want two (fp32, 4 + 4 heads: 18.2 us against 21.7).
+constexpr int kBlocks = 2;
+template <int AHEAD> constexpr int kStages = AHEAD <= 2 ? 3 : 2;
+template <typename T, int LPR, bool NEIGHBOURS, int AHEAD, Places PLACES>
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateParams p, int parts_q, int rows_per) {
+  constexpr bool ONE = PLACES == kOneKind, SIDE = PLACES == kSideBySide;
+  constexpr int HPW = 32 / LPR, HD = LPR * 8, STAGES = kStages<AHEAD>;
+  __shared__ __align__(16) Angles bufs[kThreads / 32][SIDE ? kSide : 1];
+  Angles* buf = bufs[threadIdx.x >> 5];
+  const int lane = threadIdx.x & 31, heads = p.n_heads + p.n_kv;
   const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
-  const Part part = part_of(p, blockIdx.y, heads_per, y_q);
-  const int first = part.first, last = part.last;
-  const T* in = (const T*)(part.is_q ? p.q : p.k);
-  T* out = (T*)(part.is_q ? p.q_out : p.k_out);
-  const T* g = p.norm ? (const T*)(part.is_q ? p.g_q : p.g_k) : nullptr;
-  const size_t stride = part.is_q ? p.q_stride : p.k_stride, out_stride = part.is_q ? p.qo_stride : p.ko_stride;
-  const unsigned warps = gridDim.x * (kThreads / 32), rows = p.rows;
-  unsigned row = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const unsigned rows = p.rows, step = gridDim.x * (kThreads / 32) * (SIDE ? rows_per : 1);
+  unsigned row = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * (SIDE ? rows_per : 1);
   if (row >= rows) return;
-  // the u-th head of a batch that begins at h0, from the row's start (its elements are read and written once each, so q_out may be q)
-  auto at = [&](int h0, int u) { return WHOLE ? (h0 + hl) * HD + u * HPW * HD : min(h0 + hl + u * HPW, last - 1) * HD; };
-  Runs<T> x[AHEAD], next[AHEAD];
-  auto load = [&](Runs<T> (&to)[AHEAD], unsigned r, int h0) {
-    const T* from = in + r * stride;
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) to[u].load(from + at(h0, u), l);
-  };
-  int pos = __ldg(p.pos + row), next_pos = 0, h0 = first;
-  const bool one = first + BATCH >= last;
+  // place u of this lane: a head of row at_row[u] of the pass, `off` elements into the row of the queries or keys (a place without one repeats the last one's, for
+  // the shuffles)
+  const bool part_q = (int)blockIdx.y < parts_q;
+  int at_row[AHEAD], off[AHEAD];
+  bool in_use[AHEAD], is_q[AHEAD];
   Runs<T> gr[AHEAD];
-  if (p.norm && g && one) {
+  const bool gains = p.norm && (p.g_q || p.g_k);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) gr[u].load(g + at(first, u), l);
-  }
-  load(x, row, h0);
-  Turn turn = angles<LPR>(p, pos, lane, buf);
-  while (true) {
-    const bool row_ends = h0 + BATCH >= last;
-    const unsigned nr = row_ends ? row + warps : row;
-    const int nh = row_ends ? first : h0 + BATCH;
-    const bool more = nr < rows && nr >= row;
-    if (more) {
-      if (row_ends) next_pos = __ldg(p.pos + nr);
-      load(next, nr, nh);
+  for (int u = 0; u < AHEAD; ++u) {
+    const int mine = lane / LPR + u * HPW;
+    at_row[u] = 0;
+    if (ONE) {
+      in_use[u] = true;
+      is_q[u] = part_q;
+      off[u] = ((part_q ? blockIdx.y : blockIdx.y - parts_q) * AHEAD * HPW + lane / LPR) * HD + u * HPW * HD;
+    } else {
+      const int place = (SIDE ? 0 : blockIdx.y * AHEAD * HPW) + mine, places = SIDE ? rows_per * heads : heads;
+      in_use[u] = place < places;
+      const int at = min(place, places - 1), hh = SIDE ? at % heads : at;
+      if (SIDE) at_row[u] = at / heads;
+      is_q[u] = hh < p.n_heads;
+      off[u] = (is_q[u] ? hh : hh - p.n_heads) * HD;
     }
-    if (pos >= 0) {
-      T* to = out + row * out_stride;
-      float r[AHEAD];
-      if (p.norm) {
-        // the gains on their way, and the heads' sums side by side: a sum alone would wait for each of its shuffles
-        if (g && !one) {
-#pragma unroll
-          for (int u = 0; u < AHEAD; ++u) gr[u].load(g + at(h0, u), l);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const Pairs y = sides<NEIGHBOURS>(x[u]);
-          r[u] = dot(y, y);
-        }
-#pragma unroll
-        for (int o = LPR / 2; o; o >>= 1)
-#pragma unroll
-          for (int u = 0; u < AHEAD; ++u) r[u] += __shfl_xor_sync(0xffffffffu, r[u], o);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) r[u] = rsqrtf(r[u] * (1.0f / HD) + p.eps);
-      }
+    const T* g = (const T*)(is_q[u] ? p.g_q : p.g_k);
+    if (p.norm && g) gr[u].load(g + off[u], l);
+    else gr[u].ones();
+  }
+  // the place's head in a row (of the pass)
+  auto head = [&](const void* q, const void* k, size_t q_stride, size_t k_stride, unsigned r, int u) {
+    if (SIDE) return (T*)(is_q[u] ? q : k) + (min(r + at_row[u], rows - 1) * (is_q[u] ? q_stride : k_stride) + off[u]);
+    T *to_q = (T*)q + r * q_stride, *to_k = (T*)k + r * k_stride;
+    return ONE ? (part_q ? to_q : to_k) + off[0] + u * HPW * HD : (is_q[u] ? to_q : to_k) + off[u];
+  };
+  extern __shared__ __align__(16) unsigned char smem[];
+  const Ring<T, AHEAD, STAGES> ring(smem, threadIdx.x >> 5, lane);
+  unsigned from_row = row;
+  auto fetch = [&](int stage) {
+    if (from_row < rows) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        Pairs y = sides<NEIGHBOURS>(x[u]);
-        if (p.norm) y = g ? times(y, times(sides<NEIGHBOURS>(gr[u]), r[u])) : times(y, r[u]);
-        y = turn.forward(y);
-        if (WHOLE || h0 + hl + u * HPW < last) store_sides<NEIGHBOURS>(to + at(h0, u), l, y);
+        const T* from = head(p.q, p.k, p.q_stride, p.k_stride, from_row, u);
+        ring.copy(stage, u, from + l.first, from + l.second);
       }
+      if (!SIDE) ring.copy_pos(stage, p.pos + from_row);
+      else if (lane < rows_per && from_row + lane < rows) ring.copy_pos(stage, p.pos + from_row + lane);      // lane i: row i of a pass
+      else ring.pos(stage) = -1;
+      from_row += step;
     }
-    if (!more) break;
-    if (row_ends) {
-      pos = next_pos;
-      turn = angles<LPR>(p, pos, lane, buf);
-    }
-    row = nr;
-    h0 = nh;
+    copy_commit();
+  };
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) x[u] = next[u];
+  for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  const Turns<LPR> turns(p, lane);
+  for (int stage = 0; row < rows; row += step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+    copy_wait<STAGES - 2>();
+    fetch(stage == 0 ? STAGES - 1 : stage - 1);
+    const int pos = ring.pos(stage);
+    if (!SIDE && pos < 0) continue;
+    Runs<T> x[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ring.get(stage, u, x[u]);
+    __syncwarp();                                                      // (the angles before are read)
+    if (SIDE) {
+      for (int i = 0; i < rows_per; ++i) turns.template make<sizeof(T) == 4>(__shfl_sync(0xffffffffu, pos, i), lane, buf[i]);
+    } else {
+      turns.template make<sizeof(T) == 4>(pos, lane, buf[0]);
+    }
+    __syncwarp();
+    Turn turn;
+    if (!SIDE) turn = Turns<LPR>::of(buf[0], lane);
+    float r[AHEAD];
+    if (p.norm) {                                                      // the heads' sums side by side: a sum alone would wait for each of its shuffles
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const Pairs y = sides<NEIGHBOURS>(x[u]);
+        r[u] = dot(y, y);
+      }
+#pragma unroll
+      for (int o = LPR / 2; o; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) r[u] += __shfl_xor_sync(0xffffffffu, r[u], o);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) r[u] = rsqrtf(r[u] * (1.0f / HD) + p.eps);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      Pairs y = sides<NEIGHBOURS>(x[u]);
+      if (p.norm) y = gains ? times(y, times(sides<NEIGHBOURS>(gr[u]), r[u])) : times(y, r[u]);
+      if (SIDE) turn = Turns<LPR>::of(buf[at_row[u]], lane);
+      y = turn.forward(y);
+      const bool used = !SIDE || __shfl_sync(0xffffffffu, pos, at_row[u]) >= 0;
+      if (used && in_use[u]) store_sides<NEIGHBOURS>(head(p.q_out, p.k_out, p.qo_stride, p.ko_stride, row, u), l, y);
+    }
   }
 }
 
@@ -247,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __gr
     gr.load(g + (size_t)h * HD, l);
     gv = sides<NEIGHBOURS>(gr);
   }
+  const Turns<LPR> turns(p, lane);
   const long long r0 = (long long)blockIdx.x * chunk, r1 = min((long long)p.rows, r0 + chunk);
   for (long long rb = r0 + warp; rb < r1; rb += ROWS) {
     // (The clamp changes no value.  Without it the compiler moves the loads behind the test of pos, and every row waits for memory twice: 120 us against 110.)
@@ -257,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __gr
     x.load(x0 + row * stride, l);
     d.load(d0 + row * gstride, l);
     if (rb >= r1 || pos < 0) continue;
-    const Turn turn = angles<LPR>(p, pos, lane, buf);
+    const Turn turn = turns.template at<true>(pos, lane, buf);
     Pairs w = turn.back(sides<NEIGHBOURS>(d));
     if (p.norm) {
       Pairs y = sides<NEIGHBOURS>(x);
@@ -309,31 +382,60 @@ Split backward_split(int heads, int hd, int rows) {
   return {chunk, (int)(((long long)rows + chunk - 1) / chunk)};
 }
 
-template <typename T, int LPR, bool NEIGHBOURS>
-cudaError_t forward_launch(const RotateParams& p, bool q, bool k, cudaStream_t s) {
-  constexpr int HPW = 32 / LPR, MOST = sizeof(T) == 2 ? 4 : 2;
-  const long long blocks = ((long long)p.rows + kThreads / 32 - 1) / (kThreads / 32);
-  const int nq = q ? p.n_heads : 0, nk = k ? p.n_kv : 0, most = max(nq, nk);
-  const int ways = (int)min((long long)ceil_div(most, HPW), max(1LL, 148 * 2 / blocks));       // at least two blocks for each SM if the heads allow it
-  const int heads_per = ceil_div(ceil_div(most, ways), HPW) * HPW, y_q = ceil_div(nq, heads_per), parts = y_q + ceil_div(nk, heads_per);
+template <typename... P, typename... A>
+cudaError_t launch_with_smem(void (*kernel)(P...), dim3 grid, int smem, cudaStream_t s, const A&... args) {
+  if (const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem); e != cudaSuccess) return e;
+  kernel<<<grid, kThreads, smem, s>>>(args...);
+  return cudaGetLastError();
+}
+template <typename T, int LPR, bool NEIGHBOURS, Places PLACES>
+cudaError_t start(const RotateParams& p, int ahead, int parts_q, int parts, int rows_per, cudaStream_t s) {
+  const long long warps = ((long long)p.rows + rows_per - 1) / rows_per, blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
   // as many blocks as the GPU holds at once: a warp goes on to its next row with that row's loads under way
   const dim3 grid((unsigned)min(blocks, (long long)max(1, 148 * kBlocks / parts)), parts);
-  auto fits = [&](int ahead) { return heads_per % (HPW * ahead) == 0 && nq % heads_per == 0 && nk % heads_per == 0; };
-  if (MOST >= 4 && fits(4)) rotate_kernel<T, LPR, NEIGHBOURS, MOST, true><<<grid, kThreads, 0, s>>>(p, heads_per, y_q);
-  else if (MOST >= 3 && fits(3)) rotate_kernel<T, LPR, NEIGHBOURS, MOST - 1, true><<<grid, kThreads, 0, s>>>(p, heads_per, y_q);
-  else if (fits(2)) rotate_kernel<T, LPR, NEIGHBOURS, 2, true><<<grid, kThreads, 0, s>>>(p, heads_per, y_q);
-  else if (fits(1)) rotate_kernel<T, LPR, NEIGHBOURS, 1, true><<<grid, kThreads, 0, s>>>(p, heads_per, y_q);
-  else rotate_kernel<T, LPR, NEIGHBOURS, 2, false><<<grid, kThreads, 0, s>>>(p, heads_per, y_q);
-  return cudaGetLastError();
+  auto go = [&](auto* kernel, int smem) { return launch_with_smem(kernel, grid, smem, s, p, parts_q, rows_per); };
+  constexpr int MOST = PLACES == kSideBySide ? 2 : kMost<T, PLACES>;
+  if constexpr (MOST >= 5) if (ahead == 5) return go(rotate_kernel<T, LPR, NEIGHBOURS, 5, PLACES>, Ring<T, 5, kStages<5>>::BLOCK);
+  if constexpr (MOST >= 4) if (ahead == 4) return go(rotate_kernel<T, LPR, NEIGHBOURS, 4, PLACES>, Ring<T, 4, kStages<4>>::BLOCK);
+  if constexpr (MOST >= 3) if (ahead == 3) return go(rotate_kernel<T, LPR, NEIGHBOURS, 3, PLACES>, Ring<T, 3, kStages<3>>::BLOCK);
+  if (ahead == 2) return go(rotate_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kStages<2>>::BLOCK);
+  return go(rotate_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kStages<1>>::BLOCK);
+}
+template <typename T, int LPR, bool NEIGHBOURS>
+cudaError_t forward_launch(const RotateParams& p, cudaStream_t s) {
+  constexpr int HPW = 32 / LPR;
+  const int heads = p.n_heads + p.n_kv, groups = ceil_div(heads, HPW);
+  const long long blocks = ((long long)p.rows + kThreads / 32 - 1) / (kThreads / 32);
+  const bool large = blocks >= 2 * 148;
+  // (1 + 1 heads, 30000 rows: 6.4 us against 29 with queries and keys in warps of their own; 2 + 2 heads 9.5 against 29)
+  if (heads <= HPW && large) return start<T, LPR, NEIGHBOURS, kSideBySide>(p, 2, 0, 1, min(kSide, 2 * HPW / heads), s);
+  // Places of a warp, by the cost of a row: about 8 for a pass and 4 for a place of it, or 5 if queries and keys share passes (their addresses take more instructions).
+  // 16 + 16 heads of 64, bf16: 44 us as one kind, 52 mixed; 16 + 4: 46 mixed, 56 in two launches of one kind each; 16 + 4 of 128: 48 in two, 52 mixed.  In small calls as few places as
+  // leave two blocks for each SM.
+  const int most = ceil_div(groups, (int)min((long long)groups, max(1LL, 148 * 2 / blocks)));
+  int mixed = 1;
+  auto mixed_cost = [&](int a) { return ceil_div(groups, a) * (5 * a + 8); };
+  for (int a = 2; a <= min(most, kMost<T, kMixed>); ++a) if (mixed_cost(a) <= mixed_cost(mixed)) mixed = a;
+  if (p.n_heads % HPW == 0 && p.n_kv % HPW == 0) {
+    const int gq = p.n_heads / HPW, gk = p.n_kv / HPW;
+    int aq = 1, ak = 1, both = 1;
+    for (int a = 2; a <= min(most, kMost<T, kOneKind>); ++a) {
+      if (gq % a == 0) aq = a;
+      if (gk % a == 0) ak = a;
+      if (gq % a == 0 && gk % a == 0) both = a;
+    }
+    const int one = groups / both * (4 * both + 8), two = large && gk ? gq / aq * (4 * aq + 8) + gk / ak * (4 * ak + 8) : INT32_MAX;
+    if (min(one, two) <= mixed_cost(mixed)) {
+      if (one <= two) return start<T, LPR, NEIGHBOURS, kOneKind>(p, both, gq / both, groups / both, 1, s);
+      const cudaError_t e = start<T, LPR, NEIGHBOURS, kOneKind>(p, aq, gq / aq, gq / aq, 1, s);
+      return e != cudaSuccess ? e : start<T, LPR, NEIGHBOURS, kOneKind>(p, ak, 0, gk / ak, 1, s);
+    }
+  }
+  return start<T, LPR, NEIGHBOURS, kMixed>(p, mixed, 0, ceil_div(groups, mixed), 1, s);
 }
 template <typename T, int LPR>
 cudaError_t forward(const RotateParams& p, cudaStream_t s) {
-  auto launch = p.neighbours ? forward_launch<T, LPR, true> : forward_launch<T, LPR, false>;
-  // Queries and keys in one launch; in two where their heads differ in number and each fills the GPU by itself, so that each has batches that fit it and
-  // neither waits for the other's longer rows (8 x 2048 rows of 16 and 4 heads: 25 us against 29).
-  if (p.n_kv == p.n_heads || p.n_kv == 0 || p.rows < 148 * kBlocks * (kThreads / 32)) return launch(p, true, p.n_kv > 0, s);
-  const cudaError_t e = launch(p, true, false, s);
-  return e != cudaSuccess ? e : launch(p, false, true, s);
+  return p.neighbours ? forward_launch<T, LPR, true>(p, s) : forward_launch<T, LPR, false>(p, s);
 }
 
 template <typename T, int LPR>
