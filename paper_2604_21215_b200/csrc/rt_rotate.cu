@@ -5,7 +5,7 @@
 // of zero.  A warp takes the heads of one row side by side: its lanes form the row's angles once, one or two each.  All products are paired fp32
 // instructions.
 // Measured on one B200, of 6.55 TB/s: 8 x 4050 rows of 16 + 16 heads of 64 with gains, bf16 44 us (92 %), fp32 89 %; 8 + 8 heads of 128 93 %, 16 + 4 of 64 89 %, 16 + 4 of 128 84 %,
-// 4 + 4 of 64 57 % in bf16 (angles and addresses of a short row), 100 % in fp32.  Gradients 111 us (91 %), heads of 128 64 %.
+// 4 + 4 of 64 57 % in bf16 (angles and addresses of a short row), 100 % in fp32.  Gradients 111 us (91 %), 8 + 8 heads of 128 113 us (90 %), 16 + 4 of 128 92 %.
 #include "rt_paged.h"
 #include "rt_tc.cuh"
 
@@ -13,13 +13,6 @@ namespace rt {
 namespace {
 
 constexpr int kThreads = 256;
-
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
 
 // Lane c of a row holds pairs 4 c .. 4 c + 3.  Its two runs of 4 elements begin at first and second; a and b of a pair are the i-th elements of the
 // two runs (halves, where rotated), or neighbours inside a run.
@@ -185,50 +178,69 @@ constexpr int kSide = 4;                                                        
 // passes a row: 45.7 us; 24 warps 46.4, 32 47.0; with two on their way 45.9, 49, 55; with the pass in registers instead of the ring 51).  Small passes want two (fp32, 4 + 4 heads: 18.2 us against 21.7).
 constexpr int kBlocks = 2;
 template <int AHEAD> constexpr int kStages = AHEAD <= 2 ? 3 : 2;
+// Backward: two places a lane, one pass on its way (16 + 16 heads of 64, bf16: 111 us; three places 119, four 114; with two passes on their way 120).
+constexpr int kBackMost = 2, kBackStages = 2;
+// The places of a lane: u is a head of row at_row[u] of the pass, `off` elements into the row of the queries or keys (a place without one repeats the last one's, for
+// the shuffles).
+template <int LPR, int AHEAD, Places PLACES> struct Line {
+  static constexpr bool ONE = PLACES == kOneKind, SIDE = PLACES == kSideBySide;
+  static constexpr int HPW = 32 / LPR, HD = LPR * 8;
+  int at_row[AHEAD], off[AHEAD];
+  bool in_use[AHEAD], is_q[AHEAD], part_q;
+  unsigned rows;
+  __device__ __forceinline__ Line(const RotateParams& p, int parts_q, int rows_per, int lane) : part_q((int)blockIdx.y < parts_q), rows(p.rows) {
+    const int heads = p.n_heads + p.n_kv;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int mine = lane / LPR + u * HPW;
+      at_row[u] = 0;
+      if (ONE) {
+        in_use[u] = true;
+        is_q[u] = part_q;
+        off[u] = ((part_q ? blockIdx.y : blockIdx.y - parts_q) * AHEAD * HPW + lane / LPR) * HD + u * HPW * HD;
+      } else {
+        const int place = (SIDE ? 0 : blockIdx.y * AHEAD * HPW) + mine, places = SIDE ? rows_per * heads : heads;
+        in_use[u] = place < places;
+        const int at = min(place, places - 1), hh = SIDE ? at % heads : at;
+        if (SIDE) at_row[u] = at / heads;
+        is_q[u] = hh < p.n_heads;
+        off[u] = (is_q[u] ? hh : hh - p.n_heads) * HD;
+      }
+    }
+  }
+  // the place's head in row r (of the pass that begins with row r)
+  template <typename E>
+  __device__ __forceinline__ E* head(const void* q, const void* k, size_t q_stride, size_t k_stride, unsigned r, int u) const {
+    if (SIDE) return (E*)(is_q[u] ? q : k) + (min(r + at_row[u], rows - 1) * (is_q[u] ? q_stride : k_stride) + off[u]);
+    E *to_q = (E*)q + r * q_stride, *to_k = (E*)k + r * k_stride;
+    return ONE ? (part_q ? to_q : to_k) + off[0] + u * HPW * HD : (is_q[u] ? to_q : to_k) + off[u];
+  }
+  template <typename T>
+  __device__ __forceinline__ void gains(const RotateParams& p, const Lane& l, Runs<T> (&gr)[AHEAD]) const {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const T* g = (const T*)(is_q[u] ? p.g_q : p.g_k);
+      if (p.norm && g) gr[u].load(g + off[u], l);
+      else gr[u].ones();
+    }
+  }
+};
+
 template <typename T, int LPR, bool NEIGHBOURS, int AHEAD, Places PLACES>
 __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateParams p, int parts_q, int rows_per) {
-  constexpr bool ONE = PLACES == kOneKind, SIDE = PLACES == kSideBySide;
-  constexpr int HPW = 32 / LPR, HD = LPR * 8, STAGES = kStages<AHEAD>;
+  constexpr bool SIDE = PLACES == kSideBySide;
+  constexpr int HD = LPR * 8, STAGES = kStages<AHEAD>;
   __shared__ __align__(16) Angles bufs[kThreads / 32][SIDE ? kSide : 1];
   Angles* buf = bufs[threadIdx.x >> 5];
-  const int lane = threadIdx.x & 31, heads = p.n_heads + p.n_kv;
+  const int lane = threadIdx.x & 31;
   const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
   const unsigned rows = p.rows, step = gridDim.x * (kThreads / 32) * (SIDE ? rows_per : 1);
   unsigned row = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * (SIDE ? rows_per : 1);
   if (row >= rows) return;
-  // place u of this lane: a head of row at_row[u] of the pass, `off` elements into the row of the queries or keys (a place without one repeats the last one's, for
-  // the shuffles)
-  const bool part_q = (int)blockIdx.y < parts_q;
-  int at_row[AHEAD], off[AHEAD];
-  bool in_use[AHEAD], is_q[AHEAD];
-  Runs<T> gr[AHEAD];
+  const Line<LPR, AHEAD, PLACES> line(p, parts_q, rows_per, lane);
   const bool gains = p.norm && (p.g_q || p.g_k);
-#pragma unroll
-  for (int u = 0; u < AHEAD; ++u) {
-    const int mine = lane / LPR + u * HPW;
-    at_row[u] = 0;
-    if (ONE) {
-      in_use[u] = true;
-      is_q[u] = part_q;
-      off[u] = ((part_q ? blockIdx.y : blockIdx.y - parts_q) * AHEAD * HPW + lane / LPR) * HD + u * HPW * HD;
-    } else {
-      const int place = (SIDE ? 0 : blockIdx.y * AHEAD * HPW) + mine, places = SIDE ? rows_per * heads : heads;
-      in_use[u] = place < places;
-      const int at = min(place, places - 1), hh = SIDE ? at % heads : at;
-      if (SIDE) at_row[u] = at / heads;
-      is_q[u] = hh < p.n_heads;
-      off[u] = (is_q[u] ? hh : hh - p.n_heads) * HD;
-    }
-    const T* g = (const T*)(is_q[u] ? p.g_q : p.g_k);
-    if (p.norm && g) gr[u].load(g + off[u], l);
-    else gr[u].ones();
-  }
-  // the place's head in a row (of the pass)
-  auto head = [&](const void* q, const void* k, size_t q_stride, size_t k_stride, unsigned r, int u) {
-    if (SIDE) return (T*)(is_q[u] ? q : k) + (min(r + at_row[u], rows - 1) * (is_q[u] ? q_stride : k_stride) + off[u]);
-    T *to_q = (T*)q + r * q_stride, *to_k = (T*)k + r * k_stride;
-    return ONE ? (part_q ? to_q : to_k) + off[0] + u * HPW * HD : (is_q[u] ? to_q : to_k) + off[u];
-  };
+  Runs<T> gr[AHEAD];
+  line.gains(p, l, gr);
   extern __shared__ __align__(16) unsigned char smem[];
   const Ring<T, AHEAD, STAGES> ring(smem, threadIdx.x >> 5, lane);
   unsigned from_row = row;
@@ -236,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
     if (from_row < rows) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const T* from = head(p.q, p.k, p.q_stride, p.k_stride, from_row, u);
+        const T* from = line.template head<T>(p.q, p.k, p.q_stride, p.k_stride, from_row, u);
         ring.copy(stage, u, from + l.first, from + l.second);
       }
       if (!SIDE) ring.copy_pos(stage, p.pos + from_row);
@@ -284,76 +296,126 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
     for (int u = 0; u < AHEAD; ++u) {
       Pairs y = sides<NEIGHBOURS>(x[u]);
       if (p.norm) y = gains ? times(y, times(sides<NEIGHBOURS>(gr[u]), r[u])) : times(y, r[u]);
-      if (SIDE) turn = Turns<LPR>::of(buf[at_row[u]], lane);
+      if (SIDE) turn = Turns<LPR>::of(buf[line.at_row[u]], lane);
       y = turn.forward(y);
-      const bool used = !SIDE || __shfl_sync(0xffffffffu, pos, at_row[u]) >= 0;
-      if (used && in_use[u]) store_sides<NEIGHBOURS>(head(p.q_out, p.k_out, p.qo_stride, p.ko_stride, row, u), l, y);
+      const bool used = !SIDE || __shfl_sync(0xffffffffu, pos, line.at_row[u]) >= 0;
+      if (used && line.in_use[u]) store_sides<NEIGHBOURS>(line.template head<T>(p.q_out, p.k_out, p.qo_stride, p.ko_stride, row, u), l, y);
     }
   }
 }
 
-// Backward: block (x, y) takes rows [x * chunk, (x + 1) * chunk) of the HPW heads that lie side by side in a warp, its warps a row each.  The gains' partial
-// sums of its rows go to part[x][heads * HD], added up by sum_parts_kernel in the order of x.
-template <typename T, int LPR, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads, 4) rotate_backward_kernel(const __grid_constant__ RotateParams p, int chunk, float* part) {
-  constexpr int HPW = 32 / LPR, HD = LPR * 8, ROWS = kThreads / 32;
-  __shared__ __align__(16) float red[ROWS][HPW * HD];
-  __shared__ __align__(16) Angles bufs[ROWS];
-  Angles& buf = bufs[threadIdx.x >> 5];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPR, hl = lane / LPR;
-  const Lane l = lane_of<NEIGHBOURS>(p, c);
-  const int heads = p.n_heads + p.n_kv, hh = blockIdx.y * HPW + hl;
-  const bool head_in = hh < heads;
-  const int hc = head_in ? hh : heads - 1;
-  const bool is_q = hc < p.n_heads;
-  const int h = is_q ? hc : hc - p.n_heads;
-  const long long stride = is_q ? p.q_stride : p.k_stride, gstride = (long long)(is_q ? p.n_heads : p.n_kv) * HD;
-  const T* x0 = (const T*)(is_q ? p.q : p.k) + (size_t)h * HD;
-  const float* d0 = (is_q ? p.dq_out : p.dk_out) + (size_t)h * HD;
-  float* o0 = (is_q ? p.dq : p.dk) + (size_t)h * HD;
-  const T* g = p.norm ? (const T*)(is_q ? p.g_q : p.g_k) : nullptr;
-  const F2 zero = f2(0.f, 0.f), one = f2(1.f, 1.f);
-  Pairs gv = {{one, one}, {one, one}}, dg = {{zero, zero}, {zero, zero}};
-  if (g) {
-    Runs<T> gr;
-    gr.load(g + (size_t)h * HD, l);
-    gv = sides<NEIGHBOURS>(gr);
-  }
-  const Turns<LPR> turns(p, lane);
-  const long long r0 = (long long)blockIdx.x * chunk, r1 = min((long long)p.rows, r0 + chunk);
-  for (long long rb = r0 + warp; rb < r1; rb += ROWS) {
-    // (The clamp changes no value.  Without it the compiler moves the loads behind the test of pos, and every row waits for memory twice: 120 us against 110.)
-    const size_t row = (size_t)min(rb, r1 - 1);
-    const int pos = __ldg(p.pos + row);
-    Runs<T> x;
-    Runs<float> d;
-    x.load(x0 + row * stride, l);
-    d.load(d0 + row * gstride, l);
-    if (rb >= r1 || pos < 0) continue;
-    const Turn turn = turns.template at<true>(pos, lane, buf);
-    Pairs w = turn.back(sides<NEIGHBOURS>(d));
-    if (p.norm) {
-      Pairs y = sides<NEIGHBOURS>(x);
-      const float r = rsqrtf(row_sum<LPR>(dot(y, y)) * (1.0f / HD) + p.eps);
-      y = times(y, r);
-      add_to(dg, w, y);
-      w = times(w, gv);
-      const float mean = row_sum<LPR>(dot(w, y)) * (1.0f / HD);
-      const Pairs m = {{f2(-mean, -mean), f2(-mean, -mean)}, {f2(-mean, -mean), f2(-mean, -mean)}};
-      add_to(w, y, m);
-      w = times(w, r);
+// Backward, the same way: w = the output's gradient turned back, y = x / rms;  dx = (w g - y mean(w g y)) / rms,  dg = sum over the rows of w y.  Both of a head's sums
+// (x^2 and w g x) go through the shuffles together.  A lane adds up dg of its places over its rows; the block's warps are added up at the end and go to
+// part[x][heads * HD], which sum_parts_kernel adds up in the order of x.
+template <typename T, int LPR, bool NEIGHBOURS, int AHEAD, Places PLACES>
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_backward_kernel(const __grid_constant__ RotateParams p, int parts_q, int rows_per, float* part) {
+  constexpr bool SIDE = PLACES == kSideBySide;
+  constexpr int HPW = 32 / LPR, HD = LPR * 8, STAGES = kBackStages, WARPS = kThreads / 32;
+  __shared__ __align__(16) Angles bufs[WARPS][SIDE ? kSide : 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads = p.n_heads + p.n_kv;
+  Angles* buf = bufs[warp];
+  const Lane l = lane_of<NEIGHBOURS>(p, lane % LPR);
+  const unsigned rows = p.rows, step = gridDim.x * WARPS * (SIDE ? rows_per : 1);
+  unsigned row = (blockIdx.x * WARPS + warp) * (SIDE ? rows_per : 1), from_row = row;
+  const Line<LPR, AHEAD, PLACES> line(p, parts_q, rows_per, lane);
+  const size_t dq_stride = (size_t)p.n_heads * HD, dk_stride = (size_t)p.n_kv * HD;
+  Runs<T> gr[AHEAD];
+  line.gains(p, l, gr);
+  extern __shared__ __align__(16) unsigned char smem[];
+  const Ring<T, AHEAD, STAGES> xs(smem, warp, lane);
+  const Ring<float, AHEAD, STAGES> ds(smem + Ring<T, AHEAD, STAGES>::BLOCK, warp, lane);
+  auto fetch = [&](int stage) {
+    if (from_row < rows) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const T* x = line.template head<T>(p.q, p.k, p.q_stride, p.k_stride, from_row, u);
+        const float* d = line.template head<float>(p.dq_out, p.dk_out, dq_stride, dk_stride, from_row, u);
+        xs.copy(stage, u, x + l.first, x + l.second);
+        ds.copy(stage, u, d + l.first, d + l.second);
+      }
+      if (!SIDE) xs.copy_pos(stage, p.pos + from_row);
+      else if (lane < rows_per && from_row + lane < rows) xs.copy_pos(stage, p.pos + from_row + lane);
+      else xs.pos(stage) = -1;
+      from_row += step;
     }
-    if (head_in) store_sides<NEIGHBOURS>(o0 + (size_t)rb * gstride, l, w);
+    copy_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  const Turns<LPR> turns(p, lane);
+  const F2 zero = f2(0.f, 0.f);
+  Pairs dg[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) dg[u] = {{zero, zero}, {zero, zero}};
+  for (int stage = 0; row < rows; row += step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+    copy_wait<STAGES - 2>();
+    fetch(stage == 0 ? STAGES - 1 : stage - 1);
+    const int pos = xs.pos(stage);
+    if (!SIDE && pos < 0) continue;
+    __syncwarp();                                                      // (the angles before are read)
+    if (SIDE) {
+      for (int i = 0; i < rows_per; ++i) turns.template make<true>(__shfl_sync(0xffffffffu, pos, i), lane, buf[i]);
+    } else {
+      turns.template make<true>(pos, lane, buf[0]);
+    }
+    __syncwarp();
+    Turn turn;
+    if (!SIDE) turn = Turns<LPR>::of(buf[0], lane);
+    Runs<T> x[AHEAD];
+    Pairs w[AHEAD];
+    float xx[AHEAD], wx[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      Runs<float> d;
+      xs.get(stage, u, x[u]);
+      ds.get(stage, u, d);
+      if (SIDE) turn = Turns<LPR>::of(buf[line.at_row[u]], lane);
+      w[u] = turn.back(sides<NEIGHBOURS>(d));
+      if (p.norm) {
+        const Pairs y = sides<NEIGHBOURS>(x[u]);
+        xx[u] = dot(y, y);
+        wx[u] = dot(times(w[u], sides<NEIGHBOURS>(gr[u])), y);
+      }
+    }
+    if (p.norm) {
+#pragma unroll
+      for (int o = LPR / 2; o; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          xx[u] += __shfl_xor_sync(0xffffffffu, xx[u], o);
+          wx[u] += __shfl_xor_sync(0xffffffffu, wx[u], o);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const bool used = !SIDE || __shfl_sync(0xffffffffu, pos, line.at_row[u]) >= 0;
+      if (!used || !line.in_use[u]) continue;
+      if (p.norm) {
+        const float r = rsqrtf(xx[u] * (1.0f / HD) + p.eps), mean = -(wx[u] * r) * (1.0f / HD);
+        const Pairs y = times(sides<NEIGHBOURS>(x[u]), r), m = {{f2(mean, mean), f2(mean, mean)}, {f2(mean, mean), f2(mean, mean)}};
+        add_to(dg[u], w[u], y);
+        w[u] = times(w[u], sides<NEIGHBOURS>(gr[u]));
+        add_to(w[u], y, m);
+        w[u] = times(w[u], r);
+      }
+      store_sides<NEIGHBOURS>(line.template head<float>(p.dq, p.dk, dq_stride, dk_stride, row, u), l, w[u]);
+    }
   }
   if (!part) return;
-  store_sides<NEIGHBOURS>(&red[warp][hl * HD], l, dg);
-  __syncthreads();
-  for (int i = threadIdx.x; i < HPW * HD; i += kThreads) {
-    if (blockIdx.y * HPW + i / HD >= heads) continue;
-    float a = 0.f;
+  copy_wait<0>();
+  __syncthreads();                                                     // (the ring is used up: it holds the warps' sums)
+  float* red = reinterpret_cast<float*>(smem);
+  constexpr int PLACE_FLOATS = AHEAD * HPW * HD;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) a += red[r][i];
-    part[(size_t)blockIdx.x * heads * HD + (size_t)blockIdx.y * HPW * HD + i] = a;
+  for (int u = 0; u < AHEAD; ++u) store_sides<NEIGHBOURS>(red + warp * PLACE_FLOATS + (u * HPW + lane / LPR) * HD, l, dg[u]);
+  __syncthreads();
+  const int first = SIDE ? 0 : (int)blockIdx.y * AHEAD * HPW, last = SIDE ? heads : min(heads, first + AHEAD * HPW);
+  for (int i = threadIdx.x; i < (last - first) * HD; i += kThreads) {
+    float a = 0.f;
+    for (int side = 0; side < (SIDE ? rows_per : 1); ++side)
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) a += red[w * PLACE_FLOATS + side * heads * HD + i];
+    part[(size_t)blockIdx.x * heads * HD + first * HD + i] = a;
   }
 }
 
@@ -373,14 +435,8 @@ __global__ void __launch_bounds__(kThreads) sum_parts_kernel(const float* part, 
   }
 }
 
-struct Split { int chunk, parts; };
-// about eight blocks for each SM, a multiple of 16 rows (two for each warp) each
-int backward_most_parts(int heads, int hd) { return max(1, ceil_div(148 * 8, ceil_div(heads, 256 / hd))); }
-Split backward_split(int heads, int hd, int rows) {
-  const int want = backward_most_parts(heads, hd);
-  const int chunk = (int)align_up((size_t)max((int)(((long long)rows + want - 1) / want), 1), 16);
-  return {chunk, (int)(((long long)rows + chunk - 1) / chunk)};
-}
+// Blocks of the backward pass along the rows, at most: two rows for each warp or more.
+int backward_blocks(int rows) { return (int)min(148LL * kBlocks, ((long long)rows + 15) / 16); }
 
 template <typename... P, typename... A>
 cudaError_t launch_with_smem(void (*kernel)(P...), dim3 grid, int smem, cudaStream_t s, const A&... args) {
@@ -438,21 +494,43 @@ cudaError_t forward(const RotateParams& p, cudaStream_t s) {
   return p.neighbours ? forward_launch<T, LPR, true>(p, s) : forward_launch<T, LPR, false>(p, s);
 }
 
+template <typename T, int LPR, bool NEIGHBOURS, Places PLACES>
+cudaError_t start_backward(const RotateParams& p, int ahead, int parts_q, int parts, int blocks, int rows_per, float* part, cudaStream_t s) {
+  auto go = [&](auto* kernel, int smem) { return launch_with_smem(kernel, dim3(blocks, parts), smem, s, p, parts_q, rows_per, part); };
+  if (ahead == 2) return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kBackStages>::BLOCK + Ring<float, 2, kBackStages>::BLOCK);
+  return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kBackStages>::BLOCK + Ring<float, 1, kBackStages>::BLOCK);
+}
+// -> the blocks along the rows, whose partial sums there are
+template <typename T, int LPR, bool NEIGHBOURS>
+cudaError_t backward(const RotateParams& p, float* part, int* blocks, cudaStream_t s) {
+  constexpr int HPW = 32 / LPR;
+  const int heads = p.n_heads + p.n_kv, groups = ceil_div(heads, HPW), all = backward_blocks(p.rows);
+  const bool large = all == 148 * kBlocks;
+  // (100000 rows of 1 + 1 heads, fp32: 29 us against 55 with queries and keys in places of their own)
+  if (heads <= HPW && large) {
+    const int side = min(kSide, 2 * HPW / heads);
+    *blocks = min(all, ceil_div(ceil_div(p.rows, side), kThreads / 32));
+    return start_backward<T, LPR, NEIGHBOURS, kSideBySide>(p, 2, 0, 1, *blocks, side, part, s);
+  }
+  // two places of a lane, by the passes that they save; one in small calls.  (4 + 4 heads of 64, bf16: 52 us mixed, 65 with a pass for each kind)
+  const int most = min(kBackMost, ceil_div(groups, min(groups, max(1, 148 * kBlocks / all))));
+  const int mixed = most == 2 && ceil_div(groups, 2) * 16 <= groups * 12 ? 2 : 1;
+  const bool whole = p.n_heads % HPW == 0 && p.n_kv % HPW == 0;
+  if (whole && p.n_heads / HPW % mixed == 0 && p.n_kv / HPW % mixed == 0) {
+    *blocks = min(all, max(1, 148 * kBlocks * mixed / groups));
+    return start_backward<T, LPR, NEIGHBOURS, kOneKind>(p, mixed, p.n_heads / HPW / mixed, groups / mixed, *blocks, 1, part, s);
+  }
+  *blocks = min(all, max(1, 148 * kBlocks / ceil_div(groups, mixed)));
+  return start_backward<T, LPR, NEIGHBOURS, kMixed>(p, mixed, 0, ceil_div(groups, mixed), *blocks, 1, part, s);
+}
 template <typename T, int LPR>
-cudaError_t backward(const RotateParams& p, const Split& sp, float* part, cudaStream_t s) {
-  const dim3 grid(sp.parts, ceil_div(p.n_heads + p.n_kv, 32 / LPR));
-  if (p.neighbours) rotate_backward_kernel<T, LPR, true><<<grid, kThreads, 0, s>>>(p, sp.chunk, part);
-  else rotate_backward_kernel<T, LPR, false><<<grid, kThreads, 0, s>>>(p, sp.chunk, part);
-  return cudaGetLastError();
+cudaError_t backward(const RotateParams& p, float* part, int* blocks, cudaStream_t s) {
+  return p.neighbours ? backward<T, LPR, true>(p, part, blocks, s) : backward<T, LPR, false>(p, part, blocks, s);
 }
 
 }  // namespace
 
-size_t rotate_backward_workspace(int heads, int hd, int rows) {
-  // (no fewer parts for more rows, so that a workspace for many rows serves fewer)
-  const int most = backward_most_parts(heads, hd), parts = rows / 16 + 1;
-  return align_up((size_t)(parts < most ? parts : most) * heads * hd * 4, 256);
-}
+size_t rotate_backward_workspace(int heads, int hd, int rows) { return align_up((size_t)max(1, backward_blocks(rows)) * heads * hd * 4, 256); }
 
 cudaError_t rotate_launch(int dtype, const RotateParams& p, cudaStream_t s) {
   if (dtype == RT_BF16) return p.hd == 64 ? forward<__nv_bfloat16, 8>(p, s) : forward<__nv_bfloat16, 16>(p, s);
@@ -461,16 +539,16 @@ cudaError_t rotate_launch(int dtype, const RotateParams& p, cudaStream_t s) {
 
 cudaError_t rotate_backward_launch(int dtype, const RotateParams& p, void* workspace, cudaStream_t s) {
   const int heads = p.n_heads + p.n_kv;
-  const Split sp = backward_split(heads, p.hd, p.rows);
+  int blocks = 0;
   float* part = (p.dg_q || p.dg_k) ? (float*)workspace : nullptr;
   if (p.rows > 0) {
     cudaError_t e;
-    if (dtype == RT_BF16) e = p.hd == 64 ? backward<__nv_bfloat16, 8>(p, sp, part, s) : backward<__nv_bfloat16, 16>(p, sp, part, s);
-    else e = p.hd == 64 ? backward<float, 8>(p, sp, part, s) : backward<float, 16>(p, sp, part, s);
+    if (dtype == RT_BF16) e = p.hd == 64 ? backward<__nv_bfloat16, 8>(p, part, &blocks, s) : backward<__nv_bfloat16, 16>(p, part, &blocks, s);
+    else e = p.hd == 64 ? backward<float, 8>(p, part, &blocks, s) : backward<float, 16>(p, part, &blocks, s);
     if (e != cudaSuccess) return e;
   }
   if (!part) return cudaSuccess;
-  return launch_chained(sum_parts_kernel, dim3(ceil_div(heads * p.hd, 32)), dim3(kThreads), 0, s, p.rows > 0, (const float*)part, p.rows > 0 ? sp.parts : 0,
+  return launch_chained(sum_parts_kernel, dim3(ceil_div(heads * p.hd, 32)), dim3(kThreads), 0, s, p.rows > 0, (const float*)part, blocks,
                         p.n_heads * p.hd, heads * p.hd, p.dg_q, p.dg_k);
 }
 
