@@ -114,8 +114,9 @@ void rotate_fill(const rt_rotate_config* c, RotateParams* p) {
   p->eps = c->rms_eps;
   for (int i = 0; i < c->rot_dim / 2; ++i) {
     double t = c->freq[i] / 6.283185307179586476925286766559;
-    t -= rint(t);                                                             // (exact)
-    const unsigned long long n = (unsigned long long)ldexp(fabs(t), 64);      // at most 2^63
+    constexpr double kWhole = 6755399441055744.0;                             // 1.5 * 2^52: adding it rounds to a whole number (rint is a call, and there are up to 64)
+    t -= fabs(t) < 1e15 ? (t + kWhole) - kWhole : rint(t);                     // (exact)
+    const unsigned long long n = (unsigned long long)(fabs(t) * 18446744073709551616.0);      // 2^64 of them a turn; at most 2^63
     p->turns[i] = t < 0 ? 0 - n : n;
   }
 }
