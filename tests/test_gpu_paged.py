@@ -605,6 +605,57 @@ def test_gradients_of_the_rotation(case, dtype):
             assert ((dg.double() - ref).abs() <= err.detach()).all()
 
 
+# rows side by side in a warp (an odd number of them, no keys, both sizes of heads), queries and keys in one pass, in launches of their own, and calls of a few hundred rows
+SHAPED_ROTATIONS = [
+    (7001, 1, 1, 64, 64, "halves", True, True),
+    (4999, 1, 0, 64, 32, "neighbours", True, True),
+    (3001, 1, 1, 128, 128, "neighbours", True, False),
+    (2503, 2, 0, 128, 64, "halves", False, False),
+    (6005, 3, 1, 64, 64, "halves", True, True),
+    (2501, 16, 4, 64, 64, "halves", True, True),
+    (2501, 16, 4, 128, 128, "halves", True, True),
+    (2402, 5, 2, 128, 128, "neighbours", True, True),
+    (700, 16, 16, 64, 64, "halves", True, True),
+    (900, 20, 20, 64, 48, "neighbours", True, True),
+    (301, 7, 6, 128, 128, "halves", True, True),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", SHAPED_ROTATIONS)
+def test_rotation_and_gradients_of_every_shape_of_pass(case, dtype):
+    test_rotation_of_normed_queries_and_keys(case, dtype)
+    test_gradients_of_the_rotation(case, dtype)
+    # in place, with rows that are not in use
+    op, q, k, pos, gq, gk, _ = rotation(case, dtype, seed=3)
+    qo, ko = op.forward(q, k, pos, gq, gk)
+    skip = torch.rand(case[0], generator=gen(5), device="cuda") < 0.3
+    q2, k2 = q.clone(), None if k is None else k.clone()
+    op.forward(q2, k2, torch.where(skip, -1, pos), gq, gk, q_out=q2, k_out=k2)
+    for got, out, x in ((q2, qo, q), (k2, ko, k)):
+        if x is not None:
+            want = out.clone()
+            want[skip] = x[skip]
+            assert torch.equal(got, want)
+
+
+def test_gains_of_queries_or_keys_alone_and_far_positions():
+    for case in ((3000, 2, 2, 64, 64, "halves", True, True), (2500, 4, 4, 64, 64, "halves", True, True), (40, 4, 4, 64, 64, "neighbours", True, True)):
+        op, q, k, pos, gq, gk, freq = rotation(case, "f32", seed=8)
+        pos[:3] = torch.tensor([2 ** 31 - 1, 2 ** 31 - 2, 1], device="cuda", dtype=torch.int32)
+        ones = torch.ones_like(gq)
+        for a, b in ((gq, None), (None, gk)):
+            got = op.forward(q, k, pos, a, b)
+            want = op.forward(q, k, pos, ones if a is None else a, ones if b is None else b)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        y = turned(q.double(), pos, freq, 0, "halves", True, gq.double())
+        ref = turned(q.double(), pos, freq, 64, case[5], True, gq.double())
+        got = op.forward(q, k, pos, gq, None)[0]
+        # far positions: 64-bit turns are off by 2^-53 of themselves, 2^31 of them by 2^-22 turns and less: 2^-19 of the pair's size
+        err = pair_size(y, 64, case[5]) * ((64 / 2 + 24) * U + 2.0 ** -19)
+        assert ((got.double() - ref).abs() <= HALF_STEP["f32"] * ref.abs() + 2 * err).all()
+
+
 def test_gradients_of_the_rotation_against_differences():
     case = (3, 2, 1, 64, 32, "halves", True, True)
     op, q, k, pos, gq, gk, freq = rotation(case, "f32", seed=6)
