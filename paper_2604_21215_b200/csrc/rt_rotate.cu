@@ -156,14 +156,6 @@ template <int LPR> struct Turns {                                      // of thi
     const float4 c = reinterpret_cast<const float4*>(buf.cos)[lane % LPR], s = reinterpret_cast<const float4*>(buf.sin)[lane % LPR];
     return {{f2(c.x, c.y), f2(c.z, c.w)}, {f2(s.x, s.y), f2(s.z, s.w)}, {f2(-s.x, -s.y), f2(-s.z, -s.w)}};
   }
-  // one row's, all lanes of the warp together
-  template <bool EXACT>
-  __device__ __forceinline__ Turn at(int pos, int lane, Angles& buf) const {
-    __syncwarp();                                                      // (what was there is read)
-    make<EXACT>(pos, lane, buf);
-    __syncwarp();
-    return of(buf, lane);
-  }
 };
 
 // Forward.  The heads of a row, queries' first, then keys', are a line; a warp has AHEAD * 32 / LPR places and goes from row to row.
@@ -180,6 +172,7 @@ constexpr int kBlocks = 2;
 template <int AHEAD> constexpr int kStages = AHEAD <= 2 ? 3 : 2;
 // Backward: two places a lane, one pass on its way (16 + 16 heads of 64, bf16: 111 us; three places 119, four 114; with two passes on their way 120).
 constexpr int kBackMost = 2, kBackStages = 2;
+
 // The places of a lane: u is a head of row at_row[u] of the pass, `off` elements into the row of the queries or keys (a place without one repeats the last one's, for
 // the shuffles).
 template <int LPR, int AHEAD, Places PLACES> struct Line {
@@ -454,8 +447,8 @@ cudaError_t start(const RotateParams& p, int ahead, int parts_q, int parts, int 
   if constexpr (MOST >= 5) if (ahead == 5) return go(rotate_kernel<T, LPR, NEIGHBOURS, 5, PLACES>, Ring<T, 5, kStages<5>>::BLOCK);
   if constexpr (MOST >= 4) if (ahead == 4) return go(rotate_kernel<T, LPR, NEIGHBOURS, 4, PLACES>, Ring<T, 4, kStages<4>>::BLOCK);
   if constexpr (MOST >= 3) if (ahead == 3) return go(rotate_kernel<T, LPR, NEIGHBOURS, 3, PLACES>, Ring<T, 3, kStages<3>>::BLOCK);
-  if (ahead == 2) return go(rotate_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kStages<2>>::BLOCK);
-  return go(rotate_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kStages<1>>::BLOCK);
+  if constexpr (PLACES != kSideBySide) if (ahead == 1) return go(rotate_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kStages<1>>::BLOCK);
+  return go(rotate_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kStages<2>>::BLOCK);
 }
 template <typename T, int LPR, bool NEIGHBOURS>
 cudaError_t forward_launch(const RotateParams& p, cudaStream_t s) {
@@ -497,8 +490,9 @@ cudaError_t forward(const RotateParams& p, cudaStream_t s) {
 template <typename T, int LPR, bool NEIGHBOURS, Places PLACES>
 cudaError_t start_backward(const RotateParams& p, int ahead, int parts_q, int parts, int blocks, int rows_per, float* part, cudaStream_t s) {
   auto go = [&](auto* kernel, int smem) { return launch_with_smem(kernel, dim3(blocks, parts), smem, s, p, parts_q, rows_per, part); };
-  if (ahead == 2) return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kBackStages>::BLOCK + Ring<float, 2, kBackStages>::BLOCK);
-  return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kBackStages>::BLOCK + Ring<float, 1, kBackStages>::BLOCK);
+  if constexpr (PLACES != kSideBySide)
+    if (ahead == 1) return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 1, PLACES>, Ring<T, 1, kBackStages>::BLOCK + Ring<float, 1, kBackStages>::BLOCK);
+  return go(rotate_backward_kernel<T, LPR, NEIGHBOURS, 2, PLACES>, Ring<T, 2, kBackStages>::BLOCK + Ring<float, 2, kBackStages>::BLOCK);
 }
 // -> the blocks along the rows, whose partial sums there are
 template <typename T, int LPR, bool NEIGHBOURS>
