@@ -214,24 +214,16 @@ struct Mma {
   static constexpr bool F8 = sizeof(CT) == 1;
   static constexpr int KS = HD / 16, NT = S::KT / 8, KPL = S::KT / 4, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
   unsigned q[TERMS][KS][2];
-  float o[HD / 8][4];
+  F2 o[HD / 8];                            // columns 2 c and 2 c + 1 of every output tile, both terms of the weights together
   float m, mv, q_scale;                    // running maximum (log2 units), that of the scaled weights (F8)
   F2 l;                                    // this lane's part of the sum
   float slope;
 
-  // Where a product of weights and values adds up.  The tensor core cuts what a sum loses instead of rounding it, which over thousands of
-  // positions would show in an fp32 output (up to n / 16 half steps): there the products of 16 positions are added with ordinary sums.
-  struct Out {
-    float c[4];
-    __device__ __forceinline__ Out(const float (&o)[4]) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c[e] = QF32 ? 0.f : o[e];
-    }
-    __device__ __forceinline__ void add(float (&o)[4]) const {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = QF32 ? o[e] + c[e] : c[e];
-    }
-  };
+  // The tensor core cuts what a sum loses instead of rounding it: an accumulator kept over a long piece loses half a step of 2^-23 with every product, always
+  // towards zero (16 sequences of 12 to 33 thousand pairs: 1.5e-5, where fp32 sums are off by 1e-7).  So it adds up a unit at most, CHAIN sixteens, and ordinary sums
+  // do the rest; for an fp32 output every sixteen by itself.
+  static constexpr int CHAIN = QF32 ? 1 : S::SUB;
+  __device__ __forceinline__ static F2 joined(const float (&c)[4]) { return add(f2(c[0], c[1]), f2(c[2], c[3])); }
 
   __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in, int lane) {
     const int r = lane >> 2, c = lane & 3;
@@ -278,9 +270,7 @@ struct Mma {
     m = mv = -INFINITY;
     l = f2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < HD / 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    for (int j = 0; j < HD / 8; ++j) o[j] = f2(0.f, 0.f);
   }
 
   // One staged unit: positions j0 .. j0 + KT; the first `live` count, but not the sixteens whose bit is
@@ -388,13 +378,12 @@ struct Mma {
       const float wo = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - topv)) : w;
       l = mul(l, f2(w, w));
 #pragma unroll
-      for (int j = 0; j < HD / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] *= wo;
+      for (int j = 0; j < HD / 8; ++j) o[j] = mul(o[j], f2(wo, wo));
       m = top;
       mv = topv;
     }
     const float ref = m == -INFINITY ? 0.f : -m, refv = mv == -INFINITY ? 0.f : kWeightLog2 - mv;
+    float acc[HD / 8][4];                    // what the tensor core adds up
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
       unsigned w0[2], w1[2], w2[2];          // terms of the weights of positions 4 sub + (0, 1) and (2, 3) of the lane's
@@ -427,7 +416,6 @@ struct Mma {
           }
 #pragma unroll
           for (int half = 0; half < 2; ++half) {       // four products, then the four of the third term
-            Out acc[4] = {o[8 * i + 4 * half], o[8 * i + 4 * half + 1], o[8 * i + 4 * half + 2], o[8 * i + 4 * half + 3]};
             unsigned b0[4], b1[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -435,12 +423,14 @@ struct Mma {
               const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
               b0[y] = __byte_perm(x[0][j / 2], x[1][j / 2], sel);
               b1[y] = __byte_perm(x[2][j / 2], x[3][j / 2], sel);
-              mma_bf16(acc[y].c, w0[0], w1[0], w0[1], w1[1], b0[y], b1[y]);
+              if (sub % CHAIN == 0) mma_first<false>(acc[8 * i + j], w0[0], w1[0], w0[1], w1[1], b0[y], b1[y]);
+              else mma_bf16(acc[8 * i + j], w0[0], w1[0], w0[1], w1[1], b0[y], b1[y]);
             }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-              mma_bf16(acc[y].c, w2[0], 0u, w2[1], 0u, b0[y], b1[y]);
-              acc[y].add(o[8 * i + 4 * half + y]);
+              const int t = 8 * i + 4 * half + y;
+              mma_bf16(acc[t], w2[0], 0u, w2[1], 0u, b0[y], b1[y]);
+              if (sub % CHAIN == CHAIN - 1) o[t] = add(o[t], joined(acc[t]));
             }
           }
         }
@@ -465,10 +455,11 @@ struct Mma {
             const unsigned y0 = __byte_perm(x[0][d], x[1][d], sel), y1 = __byte_perm(x[2][d], x[3][d], sel);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float (&to)[4] = o[4 * d + 2 * h + e];
-              Out acc(to);
-              mma_f16(acc.c, w0[0], w1[0], w0[1], w1[1], e4m3x2_to_h2(y0 >> (16 * e)), e4m3x2_to_h2(y1 >> (16 * e)));
-              acc.add(to);
+              const int t = 4 * d + 2 * h + e;
+              const unsigned b0 = e4m3x2_to_h2(y0 >> (16 * e)), b1 = e4m3x2_to_h2(y1 >> (16 * e));
+              if (sub % CHAIN == 0) mma_first<true>(acc[t], w0[0], w1[0], w0[1], w1[1], b0, b1);
+              else mma_f16(acc[t], w0[0], w1[0], w0[1], w1[1], b0, b1);
+              if (sub % CHAIN == CHAIN - 1) o[t] = add(o[t], joined(acc[t]));
             }
           }
         }
@@ -487,15 +478,16 @@ struct Mma {
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     const float back = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - m - kWeightLog2)) : 1.f;
 #pragma unroll
-    for (int j = 0; j < HD / 8; ++j)
+    for (int j = 0; j < HD / 8; ++j) {
+      float y[2];
+      split(mul(o[j], f2(back, back)), y[0], y[1]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         // column 2 c + e of output tile j
-        const int d = F8 ? (HD / 8) * (2 * c + e) + j : (j / 8) * 64 + 8 * (2 * c + e) + j % 8;
-        const float y = (o[j][e] + o[j][e + 2]) * back;
-        out[r * HD + d] = y;
-        all = fmaf(y, 0.f, all);           // NaN once one is not finite
+        out[r * HD + (F8 ? (HD / 8) * (2 * c + e) + j : (j / 8) * 64 + 8 * (2 * c + e) + j % 8)] = y[e];
+        all = fmaf(y[e], 0.f, all);        // NaN once one is not finite
       }
+    }
     if (c == 0) { out[kRows * HD + 2 * r] = m; out[kRows * HD + 2 * r + 1] = sum; }
     return !__any_sync(0xffffffffu, r < g_in && !(all == 0.f && sum < INFINITY));
   }

@@ -824,3 +824,40 @@ print("captured")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("cache,n", [("e4m3", 90000), ("bf16", 40000)])
+def test_sums_of_long_sequences_are_added_in_fp32(cache, n):
+    """Queries of zeros weigh all pairs alike and values are positive, so an output is the mean of its values, and its error in fp32 that of the sums: half a step for each
+    unit that a warp adds up, a few steps inside a unit, the joined parts.  (A tensor core that accumulated a whole piece would lose up to a step with every product.)
+    The bf16 output then lies between the roundings of the two ends."""
+    rt = rt_module()
+    B, H, hd, page = 8, 16, 64, 64
+    m = -(-n // page)
+    c = rt.PagedCache.empty(B * m, page, H, B, m, head_dim=hd, dtype=cache)
+    c.page_table.copy_(torch.arange(B * m).flip(0).view(B, m).int())
+    g = gen(12)
+    part = torch.rand((1, H, 1, hd), generator=g, device="cuda")        # how often a dimension is large: the means cover the steps of bf16
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    want = []
+    for b in range(B):
+        pages = slice((B - 1 - b) * m, (B - b) * m)                     # (flipped: the sequence's pages from the last to the first)
+        large = torch.rand((m, H, page, hd), generator=g, device="cuda") < part
+        e = torch.randint(-20, 1, (m, H, page), generator=g, device="cuda")
+        if cache == "e4m3":
+            c.v.view(torch.uint8)[pages] = torch.where(large, 0x3f, 0x38).to(torch.uint8)       # 1.875, 1
+            c.v_exp[pages] = (127 + e).to(torch.uint8)
+            v = torch.where(large, 1.875, 1.0).double() * (2.0 ** e.double())[..., None]
+        else:
+            v = torch.where(large, 1.9921875, 1.0) * (2.0 ** e.float())[..., None]
+            c.v[pages] = v.bfloat16()
+            v = v.double()
+        v = v.flip(0).transpose(0, 1).reshape(H, m * page, hd)[:, :n]
+        want.append(v.mean(1))
+    out = c.attend(torch.zeros((B, H, hd), dtype=torch.bfloat16, device="cuda"), lens).double()
+    o = torch.stack(want)
+    unit, warps = 64 if cache == "e4m3" else 32, 148 * 12
+    per_warp, parts = B * H * -(-n // unit) / warps, warps / (B * H) + 2
+    err = (per_warp + parts + 16 + 24) * U                              # 16: four products of a unit, four half steps each; 24: the division and the like
+    low, high = (x.float().bfloat16().double() for x in (o * (1 - err), o * (1 + err)))
+    assert ((out >= low) & (out <= high)).all(), int(((out < low) | (out > high)).sum())
