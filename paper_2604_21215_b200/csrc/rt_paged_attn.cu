@@ -23,7 +23,8 @@
 // row (an order of the contraction is free, and so is the order of the output's columns as long as the epilogue knows it): no transposition.
 //   bf16 pages: bf16 products, queries in 1 (bf16) or 3 terms (fp32), weights in 3 terms.
 //   e4m3 pages: codes are exact in fp16; fp16 products, queries (scaled by a power of two) in 1 or 2 terms, weights in 2 terms.  The keys' scales
-//   multiply the scores, the values' scales the weights, which are kept relative to the largest scaled weight so far (fp16's range).
+//   multiply the scores, the values' scales the weights, which are kept relative to the largest scaled weight so far (fp16's range); the exponent of a scale is
+//   added to a score less its row's maximum, never to the score itself, whose last bit may be worth more than the exponent.
 //   fp32 pages: CUDA cores, fp32 throughout.
 #include <cuda_fp16.h>
 
@@ -36,7 +37,7 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 8;      // warps of a block; query heads of a unit
 constexpr int kSms = 148;
-constexpr float kWeightLog2 = 15.0f;      // fp16 weights lie in [0, 2^15]: their two terms keep 2^-40 of the largest
+constexpr float kWeightLog2 = 15.0f, kWeightBack = 1.0f / 32768.0f;      // fp16 weights lie in [0, 2^15]: their two terms keep 2^-40 of the largest
 
 // ---- shapes ------------------------------------------------------------------------------------
 template <typename CT, int HD>
@@ -138,6 +139,9 @@ __device__ __forceinline__ float ex2(float x) {        // 2^x to 2^-22, 0 below 
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float whole_power(float n) {      // 2^n of a whole number below 128; 0 below 2^-126
+  return __uint_as_float((unsigned)max(127 + (int)n, 0) << 23);
+}
 __device__ __forceinline__ float q_at(int dtype, const void* p, size_t i) {
   return dtype == RT_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : ((const float*)p)[i];
 }
@@ -215,7 +219,8 @@ struct Mma {
   static constexpr int KS = HD / 16, NT = S::KT / 8, KPL = S::KT / 4, E = 16 / (int)sizeof(CT), TERMS = QF32 ? (F8 ? 2 : 3) : 1;
   unsigned q[TERMS][KS][2];
   F2 o[HD / 8];                            // columns 2 c and 2 c + 1 of every output tile, both terms of the weights together
-  float m, mv, q_scale;                    // running maximum (log2 units), that of the scaled weights (F8)
+  float m, q_scale;                        // running maximum (log2 units)
+  float top_v;                             // F8: a whole number, at least every weight times value scale (log2) so far relative to m, and less than 1 above the largest; o is relative to it
   F2 l;                                    // this lane's part of the sum
   float slope;
 
@@ -267,7 +272,7 @@ struct Mma {
         q[t][s][1] = F8 ? take_f16(x[2 * s + 1]) : take_bf16(x[2 * s + 1]);
       }
     slope = p.q.alibi_slopes ? __ldg(p.q.alibi_slopes + h0 + (in ? r : 0)) * kLog2e : 0.f;
-    m = mv = -INFINITY;
+    m = top_v = -INFINITY;
     l = f2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j) o[j] = f2(0.f, 0.f);
@@ -304,7 +309,7 @@ struct Mma {
         }
       }
     }
-    // scores in log2 units (for F8 also those of the scaled weights), the maximum of the row, weights; two positions at a time
+    // scores in log2 units, the maximum of the row (for F8 then that of the scaled weights), weights; two positions at a time
     F2 a[NT], av[F8 ? NT : 1];
     unsigned ke[KPL / 4], ve[KPL / 4];       // the exponents of this lane's positions
     if (F8) {
@@ -333,14 +338,6 @@ struct Mma {
 #pragma unroll
       for (int t = 0; t < NT; ++t) a[t] = fma(f2(slope, slope), add(f2(far, far), f2((float)(2 * t), (float)(2 * t + 1))), a[t]);
     }
-    if (F8) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {         // 2^23 + exponent - (2^23 + 127)
-        const unsigned w = ve[t / 2], sel = 0x7550u + 2 * (t & 1);
-        av[F8 ? t : 0] = add(a[t], add(f2(__uint_as_float(__byte_perm(w, 0x4b000000u, sel)), __uint_as_float(__byte_perm(w, 0x4b000000u, sel + 1))),
-                                       f2(-8388735.f, -8388735.f)));
-      }
-    }
     if (live < S::KT || bad) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -350,39 +347,49 @@ struct Mma {
         float x, y;
         split(a[t], x, y);
         a[t] = f2(i0 != 0.f ? i0 : x, i1 != 0.f ? i1 : y);
-        if (F8) {
-          split(av[F8 ? t : 0], x, y);
-          av[F8 ? t : 0] = f2(i0 != 0.f ? i0 : x, i1 != 0.f ? i1 : y);
-        }
       }
     }
-    float top = m, topv = mv;
+    float top = m;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float x, y;
       split(a[t], x, y);
       top = fmaxf(top, fmaxf(x, y));
-      if (F8) {
-        split(av[F8 ? t : 0], x, y);
-        topv = fmaxf(topv, fmaxf(x, y));
-      }
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const float ref = top == -INFINITY ? 0.f : -top, shift = m == -INFINITY ? 0.f : m - top;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) a[t] = add(a[t], f2(ref, ref));
+    float topv = top_v + shift;
     if (F8) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {         // 2^23 + exponent - (2^23 + 127)
+        const unsigned w = ve[t / 2], sel = 0x7550u + 2 * (t & 1);
+        av[F8 ? t : 0] = add(a[t], add(f2(__uint_as_float(__byte_perm(w, 0x4b000000u, sel)), __uint_as_float(__byte_perm(w, 0x4b000000u, sel + 1))),
+                                       f2(-8388735.f, -8388735.f)));
+        float x, y;
+        split(av[F8 ? t : 0], x, y);
+        topv = fmaxf(topv, fmaxf(x, y));
+      }
       topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, 1));
       topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, 2));
     }
-    if (__any_sync(0xffffffffu, top > m || (F8 && topv > mv))) {
-      const float w = m == -INFINITY ? 0.f : ex2(m - top);
-      const float wo = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - topv)) : w;
+    if (__any_sync(0xffffffffu, top > m || (F8 && topv > top_v))) {
+      const float w = m == -INFINITY ? 0.f : ex2(shift);
+      float wo = w;
+      if (F8) {                              // w 2^(top_v - to); shift + up is exact where up > 0 (up <= -shift)
+        const float to = ceilf(topv), up = top_v - to;
+        if (top_v == -INFINITY) wo = 0.f;
+        else wo = up > 0.f ? ex2(shift + up) : w * whole_power(up);
+        top_v = to;
+      }
       l = mul(l, f2(w, w));
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j) o[j] = mul(o[j], f2(wo, wo));
       m = top;
-      mv = topv;
     }
-    const float ref = m == -INFINITY ? 0.f : -m, refv = mv == -INFINITY ? 0.f : kWeightLog2 - mv;
+    const float refv = top_v == -INFINITY ? 0.f : kWeightLog2 - top_v;
     float acc[HD / 8][4];                    // what the tensor core adds up
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
@@ -390,7 +397,7 @@ struct Mma {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int t = 2 * sub + h;
-        F2 w = ex2(add(a[t], f2(ref, ref)));
+        F2 w = ex2(a[t]);
         l = add(l, w);
         if (F8) {
           w = ex2(add(av[F8 ? t : 0], f2(refv, refv)));
@@ -476,11 +483,11 @@ struct Mma {
     sum += other;
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    const float back = F8 ? (mv == -INFINITY ? 0.f : ex2(mv - m - kWeightLog2)) : 1.f;
+    const float back = top_v == -INFINITY ? 0.f : whole_power(top_v);       // (times 2^-15 it may lie below fp32's normal numbers, outputs may not)
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j) {
       float y[2];
-      split(mul(o[j], f2(back, back)), y[0], y[1]);
+      split(F8 ? mul(mul(o[j], f2(kWeightBack, kWeightBack)), f2(back, back)) : o[j], y[0], y[1]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         // column 2 c + e of output tile j

@@ -861,3 +861,36 @@ def test_sums_of_long_sequences_are_added_in_fp32(cache, n):
     err = (per_warp + parts + 16 + 24) * U                              # 16: four products of a unit, four half steps each; 24: the division and the like
     low, high = (x.float().bfloat16().double() for x in (o * (1 - err), o * (1 + err)))
     assert ((out >= low) & (out <= high)).all(), int(((out < low) | (out > high)).sum())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+def test_values_keep_their_scale_beside_scores_of_any_size(cache, hd, dtype):
+    """Scores that are whole powers of two: one pair gives its value, two pairs of one key the mean of their values however large the score and however small the values;
+    a third pair, far below, has no weight.  Weights are good to 2^-20, and the values are exact in both types of pages."""
+    rt = rt_module()
+    c = rt.PagedCache.empty(3, 16, 1, 3, 1, head_dim=hd, dtype=cache)
+    c.page_table.copy_(torch.arange(3).view(3, 1).int())
+    at = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    seq, pos = at(0, 1, 1, 2, 2, 2), at(0, 0, 1, 0, 1, 2)
+    for score in (1.0, 2.0 ** 10, 2.0 ** 17, 2.0 ** 23, -2.0 ** 24, 2.0 ** 28, -2.0 ** 28, 2.0 ** 40):
+        for e in (-120, -100, -30, -8, -3, 0, 20, 60, 110):
+            k = torch.zeros((6, 1, hd), device="cuda")
+            k[:, 0, 0] = 1.0
+            k[5, 0, 0] = -1.0 if score > 0 else 2.0                     # 2 |score| or |score| below the others
+            far = abs(score) > 200
+            v = (1.0 + torch.arange(6 * hd, device="cuda").remainder(7).float()).view(6, 1, hd) * 2.0 ** e
+            v[[2, 4]] *= 0.125                                          # (another scale)
+            v[5] *= 2.0 ** 10
+            c.write(k, v, seq, pos)
+            kr, vr = c.read(seq, pos, dtype="f32")
+            assert torch.equal(kr, k) and torch.equal(vr, v)
+            q = torch.zeros((3, 1, hd), device="cuda", dtype=TYPES[dtype])
+            q[:, 0, 0] = score
+            lse = torch.empty((3, 1), device="cuda")
+            out = c.attend(q, at(1, 2, 3 if far else 2), scale=1.0, lse=lse).double()[:, 0]
+            v = v.double()[:, 0]
+            want = torch.stack((v[0], (v[1] + v[2]) / 2, (v[3] + v[4]) / 2))
+            assert ((out - want).abs() <= (2.0 ** -20 + HALF_STEP[dtype]) * want).all(), (score, e)
+            assert ((lse.double()[:, 0] - score - torch.tensor([0.0, math.log(2.0), math.log(2.0)], device="cuda")).abs() <= 4 * U * abs(score) + 2.0 ** -20).all()
