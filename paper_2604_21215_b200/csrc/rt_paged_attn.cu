@@ -225,9 +225,10 @@ struct Mma {
   float slope;
 
   // The tensor core cuts what a sum loses instead of rounding it: an accumulator kept over a long piece loses half a step of 2^-23 with every product, always
-  // towards zero (16 sequences of 12 to 33 thousand pairs: 1.5e-5, where fp32 sums are off by 1e-7).  So it adds up a unit at most, CHAIN sixteens, and ordinary sums
-  // do the rest; for an fp32 output every sixteen by itself.
-  static constexpr int CHAIN = QF32 ? 1 : S::SUB;
+  // towards zero (16 sequences of 12 to 33 thousand pairs: 1.5e-5, where fp32 sums are off by 1e-7).  So it adds up CHAIN sixteens of positions, and ordinary sums do
+  // the rest: two over bf16 pages (their unit; 24 of 0 to 4096 33.2 us, one by one 33.7), one over e4m3 pages (16 of 12 to 33 thousand 138 us; with units of four, whose
+  // accumulators all live at once, 141.5; with the whole piece in the tensor core 130), and one for fp32 outputs.
+  static constexpr int CHAIN = F8 || QF32 ? 1 : S::SUB;
   __device__ __forceinline__ static F2 joined(const float (&c)[4]) { return add(f2(c[0], c[1]), f2(c[2], c[3])); }
 
   __device__ __forceinline__ void begin(const PagedAttnParams& p, int b, int h0, int g_in, int lane) {
@@ -390,7 +391,7 @@ struct Mma {
       m = top;
     }
     const float refv = top_v == -INFINITY ? 0.f : kWeightLog2 - top_v;
-    float acc[HD / 8][4];                    // what the tensor core adds up
+    float acc[F8 ? 1 : HD / 8][4];           // what the tensor core adds up, over bf16 pages
 #pragma unroll
     for (int sub = 0; sub < S::SUB; ++sub) {
       unsigned w0[2], w1[2], w2[2];          // terms of the weights of positions 4 sub + (0, 1) and (2, 3) of the lane's
@@ -463,10 +464,9 @@ struct Mma {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int t = 4 * d + 2 * h + e;
-              const unsigned b0 = e4m3x2_to_h2(y0 >> (16 * e)), b1 = e4m3x2_to_h2(y1 >> (16 * e));
-              if (sub % CHAIN == 0) mma_first<true>(acc[t], w0[0], w1[0], w0[1], w1[1], b0, b1);
-              else mma_f16(acc[t], w0[0], w1[0], w0[1], w1[1], b0, b1);
-              if (sub % CHAIN == CHAIN - 1) o[t] = add(o[t], joined(acc[t]));
+              float sixteen[4];
+              mma_first<true>(sixteen, w0[0], w1[0], w0[1], w1[1], e4m3x2_to_h2(y0 >> (16 * e)), e4m3x2_to_h2(y1 >> (16 * e)));
+              o[t] = add(o[t], joined(sixteen));
             }
           }
         }
