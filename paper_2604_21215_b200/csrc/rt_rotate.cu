@@ -1,8 +1,8 @@
 // qkRMS of queries and keys for each head and the rotation by the position, in one pass, and its backward pass.
 //
 // Bound: HBM traffic, if the instructions are few.  head_dim / 8 neighbouring lanes hold a row of a head; each holds the two sides a[i], b[i] of four pairs of dimensions, as
-// two loads of 4 elements, so the rotation needs no exchange and the norm a few shuffles.  Dimensions that are not rotated make pairs too, with an angle
-// of zero.  A warp takes the heads of one row side by side: its lanes form the row's angles once, one or two each.  All products are paired fp32
+// two loads of 4 elements, so the rotation needs no exchange and the norm a few shuffles.  Dimensions that are not rotated make pairs too, which stay as
+// they are.  A warp takes the heads of one row side by side: its lanes form the row's angles once, one or two each.  All products are paired fp32
 // instructions.
 // Measured on one B200, of 6.55 TB/s: 8 x 4050 rows of 16 + 16 heads of 64 with gains, bf16 44 us (92 %), fp32 89 %; 8 + 8 heads of 128 93 %, 16 + 4 of 64 89 %, 16 + 4 of 128 84 %,
 // 4 + 4 of 64 57 % in bf16 (angles and addresses of a short row), 100 % in fp32.  Gradients 111 us (91 %), 8 + 8 heads of 128 113 us (90 %), 16 + 4 of 128 92 %.
@@ -18,14 +18,14 @@ constexpr int kThreads = 256;
 // sectors (8 elements a lane in one piece take half of every sector with each access: fp32 gradients of 26775 rows of 16 + 16 heads 141 us against 109).
 // Halves: a and b of a pair are the i-th elements of the two runs; lane c holds pairs 4 c .. 4 c + 3, and what is not rotated makes pairs across its own halves.
 // Neighbours: pairs lie inside the runs; lane c holds pairs 2 c, 2 c + 1 and those HD / 4 further.
-struct Lane { int first, second; };
+struct Lane { int first, second; bool turned[2], part; };      // turned: whether pairs 0, 1 and pairs 2, 3 are rotated (rot is a multiple of 16); part: not all of a head is
 template <int LPR, bool NEIGHBOURS>
 __device__ __forceinline__ Lane lane_of(const RotateParams& p, int c) {
   constexpr int HD = LPR * 8;
-  if (NEIGHBOURS) return {4 * c, 4 * c + HD / 2};
-  if (8 * c < p.rot) return {4 * c, 4 * c + p.rot / 2};
+  if (NEIGHBOURS) return {4 * c, 4 * c + HD / 2, {4 * c < p.rot, 4 * c + HD / 2 < p.rot}, p.rot < HD};
+  if (8 * c < p.rot) return {4 * c, 4 * c + p.rot / 2, {true, true}, p.rot < HD};
   const int begin = p.rot / 2 + 4 * c;                                 // rot + 4 (c - rot / 8)
-  return {begin, begin + (HD - p.rot) / 2};
+  return {begin, begin + (HD - p.rot) / 2, {false, false}, true};
 }
 
 // a run of four elements as it lies in memory
@@ -123,15 +123,21 @@ __device__ __forceinline__ void add_to(Pairs& s, const Pairs& x, const Pairs& y)
   for (int i = 0; i < 2; ++i) { s.a[i] = fma(x.a[i], y.a[i], s.a[i]); s.b[i] = fma(x.b[i], y.b[i], s.b[i]); }
 }
 
-// A row's angles as a lane needs them: cos and sin of its pairs 0, 1 and 2, 3.
+// A row's angles as a lane needs them: cos and sin of its pairs 0, 1 and 2, 3.  Pairs that are not rotated stay as they are: an angle of zero would carry an
+// infinity or a NaN into the pair's other side.
 struct Turn {
   F2 c[2], s[2], ns[2];
-  __device__ __forceinline__ Pairs forward(const Pairs& x) const {
-    return {{fma(x.a[0], c[0], mul(x.b[0], ns[0])), fma(x.a[1], c[1], mul(x.b[1], ns[1]))}, {fma(x.a[0], s[0], mul(x.b[0], c[0])), fma(x.a[1], s[1], mul(x.b[1], c[1]))}};
+  __device__ __forceinline__ static Pairs turned(const Lane& l, const Pairs& x, const F2 (&c)[2], const F2 (&s)[2], const F2 (&ns)[2]) {
+    Pairs y = {{fma(x.a[0], c[0], mul(x.b[0], ns[0])), fma(x.a[1], c[1], mul(x.b[1], ns[1]))}, {fma(x.a[0], s[0], mul(x.b[0], c[0])), fma(x.a[1], s[1], mul(x.b[1], c[1]))}};
+    if (l.part) {                                                      // (the same for all lanes: heads that are rotated whole go past the selections; 16 + 4 heads, 7800 rows: 17.8 us, 18.3 with them)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (!l.turned[i]) { y.a[i] = x.a[i]; y.b[i] = x.b[i]; }
+    }
+    return y;
   }
-  __device__ __forceinline__ Pairs back(const Pairs& x) const {
-    return {{fma(x.a[0], c[0], mul(x.b[0], s[0])), fma(x.a[1], c[1], mul(x.b[1], s[1]))}, {fma(x.a[0], ns[0], mul(x.b[0], c[0])), fma(x.a[1], ns[1], mul(x.b[1], c[1]))}};
-  }
+  __device__ __forceinline__ Pairs forward(const Lane& l, const Pairs& x) const { return turned(l, x, c, s, ns); }
+  __device__ __forceinline__ Pairs back(const Lane& l, const Pairs& x) const { return turned(l, x, c, ns, s); }
 };
 
 // Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair through 512 bytes of shared memory of the warp's own (two loads a lane,
@@ -305,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
       Pairs y = sides<NEIGHBOURS>(x[u]);
       if (p.norm) y = gains ? times(y, times(sides<NEIGHBOURS>(gr[u]), r[u])) : times(y, r[u]);
       if (SIDE) turn = Turns<LPR>::template of<NEIGHBOURS>(buf[line.at_row[u]], lane);
-      y = turn.forward(y);
+      y = turn.forward(l, y);
       const bool used = !SIDE || __shfl_sync(0xffffffffu, pos, line.at_row[u]) >= 0;
       if (used && line.in_use[u]) store_sides<NEIGHBOURS>(line.template head<T>(p.q_out, p.k_out, p.qo_stride, p.ko_stride, row, u), l, y);
     }
@@ -378,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_backward_kernel(cons
       xs.get(stage, u, x[u]);
       ds.get(stage, u, d);
       if (SIDE) turn = Turns<LPR>::template of<NEIGHBOURS>(buf[line.at_row[u]], lane);
-      w[u] = turn.back(sides<NEIGHBOURS>(d));
+      w[u] = turn.back(l, sides<NEIGHBOURS>(d));
       if (p.norm) {
         const Pairs y = sides<NEIGHBOURS>(x[u]);
         xx[u] = dot(y, y);

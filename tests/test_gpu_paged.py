@@ -894,3 +894,61 @@ def test_values_keep_their_scale_beside_scores_of_any_size(cache, hd, dtype):
             want = torch.stack((v[0], (v[1] + v[2]) / 2, (v[3] + v[4]) / 2))
             assert ((out - want).abs() <= (2.0 ** -20 + HALF_STEP[dtype]) * want).all(), (score, e)
             assert ((lse.double()[:, 0] - score - torch.tensor([0.0, math.log(2.0), math.log(2.0)], device="cuda")).abs() <= 4 * U * abs(score) + 2.0 ** -20).all()
+
+
+def same_numbers(got, want, err):
+    """NaN and infinities where they belong, all else within err (of the finite ones)."""
+    got, fine = got.double(), torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    odd = ~fine & ~torch.isnan(want)
+    assert torch.equal(got[odd], want[odd])
+    assert ((got - want).abs() <= err)[fine].all()
+
+
+# rows side by side, queries and keys in passes of their own and mixed, small calls; nothing rotated, and parts of a head
+PARTLY_ROTATED = [(3, 1, 1, 64, 0), (40, 2, 1, 64, 32), (7001, 1, 1, 64, 16), (5000, 16, 16, 64, 32), (3700, 5, 3, 64, 48), (2402, 5, 2, 128, 64), (300, 4, 4, 128, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+@pytest.mark.parametrize("shape", PARTLY_ROTATED)
+def test_infinities_and_nan_stay_in_their_pair(shape, pairs, norm, dtype):
+    # dimensions that are not rotated have no partner; a rotated one has its own
+    R, H, kv, hd, rot = shape
+    op, q, k, pos, gq, gk, freq = rotation((R, H, kv, hd, rot, pairs, norm, norm), dtype, seed=4)
+    g = gen(6)
+    bad = torch.tensor([math.inf, -math.inf, math.nan], device="cuda")
+    for x in (q, k):
+        n = max(1, R // 50)
+        x[torch.randint(0, R, (n,), generator=g, device="cuda"), torch.randint(0, x.shape[1], (n,), generator=g, device="cuda"),
+          torch.randint(0, hd, (n,), generator=g, device="cuda")] = bad[torch.randint(0, 3, (n,), generator=g, device="cuda")].to(x.dtype)
+        x[0, 0, hd - 1] = math.inf                                      # (the last dimension, next to one that is not rotated either)
+    got = op.forward(q, k, pos, gq, gk)
+    for x, gain, y in zip((q, k), (gq, gk), got):
+        g64 = None if gain is None else gain.double()
+        want = turned(x.double(), pos, freq, rot, pairs, norm, g64)
+        err = pair_size(turned(x.double(), pos, freq, 0, pairs, norm, g64), rot, pairs) * (hd / 2 + 24) * U
+        same_numbers(y, want.to(y.dtype).double(), HALF_STEP[dtype] * 2 * (want.abs() + err) + err)
+        if not norm:
+            assert torch.equal(torch.nan_to_num(y[..., rot:]), torch.nan_to_num(x[..., rot:]))       # what is not rotated is copied
+
+    # the gradients: one infinity in some heads
+    q, k = rotation((R, H, kv, hd, rot, pairs, norm, norm), dtype, seed=4)[1:3]
+    d = [torch.randn((R, h, hd), generator=g, device="cuda") for h in (H, kv)]
+    for x in d:
+        x[0, 0, hd - 1] = math.inf
+        x[R // 2, x.shape[1] - 1, hd // 2 if rot <= hd // 2 else hd - 2] = -math.inf
+    got = op.backward(q, k, pos, d[0], d[1], gq, gk)
+    for x, gain, dy, dx, dg in zip((q, k), (gq, gk), d, got[:2], got[2:]):
+        x, w = x.double(), turned(dy.double(), -pos, freq, rot, pairs, False, None)
+        size = pair_size(torch.where(torch.isfinite(dy), dy.double(), 0.0), rot, pairs)
+        if not norm:
+            same_numbers(dx, w, size * 64 * U)
+            continue
+        r = 1 / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-6)
+        u, wg = x * r, w * gain.double().view(x.shape[1:])
+        want = r * (wg - u * (wg * u).mean(-1, keepdim=True))
+        s = size * gain.double().abs().view(x.shape[1:])
+        same_numbers(dx, want, r * (s + u.abs() * (s * u.abs()).mean(-1, keepdim=True)) * (2 * hd + 64) * U)
+        same_numbers(dg, (w * u).sum(0).reshape(-1), (size * u.abs()).sum(0).reshape(-1) * (R + hd + 64) * U)
