@@ -276,7 +276,8 @@ rt_status rt_layer_backward(const rt_config *cfg, const rt_layer_weights *w, con
  *    *status becomes RT_ERR_INVALID_ARG.  No call ever clears that word: the caller zeroes it once and
  *    reads it with rt_get_status.
  *  - The entries of the page table behind a sequence's last page are never used, positions behind its length never read.
- *  - Outputs overlap neither one another nor inputs, but where an entry point says so (RT_ERR_INVALID_ARG where that shows from addresses and strides).
+ *  - Outputs, the workspace among them, overlap neither one another nor inputs, but where an entry point says so (RT_ERR_INVALID_ARG otherwise).  Rows may lie in
+ *    turn with other rows in one array.
  *  - Strides are in elements, between the rows of consecutive tokens; a token's heads are contiguous.  Rows begin
  *    at multiples of 16 bytes and do not overlap.  Index arrays and fp32 vectors (lens, lse, slopes) need 4-byte alignment only.
  *  - The pointers belong to the device that is current. */

@@ -38,39 +38,57 @@ bool rows_ok(const void* p, int dtype, long long stride, long long row, long lon
   return rows == 1 || (stride >= row && stride <= INT64_MAX / 16 / rows && stride * esize(dtype) % 16 == 0);
 }
 
-// Whether two arrays of such rows share bytes.  Rows of one stride may lie in turn in one array (queries, keys and values of a projection); rows of two strides are
-// taken to overlap only where the arrays begin at the same place.
-bool rows_overlap(const void* a, int dtype_a, long long stride_a, long long row_a, const void* b, int dtype_b, long long stride_b, long long row_b, long long rows) {
-  if (rows == 0) return false;
-  const long long ra = row_a * esize(dtype_a), rb = row_b * esize(dtype_b), sa = rows > 1 ? stride_a * esize(dtype_a) : ra, sb = rows > 1 ? stride_b * esize(dtype_b) : rb;
-  const intptr_t pa = reinterpret_cast<intptr_t>(a), pb = reinterpret_cast<intptr_t>(b);
-  if (pa >= pb + (rows - 1) * sb + rb || pb >= pa + (rows - 1) * sa + ra) return false;
-  if (rows == 1 || (sa == ra && sb == rb)) return true;
-  if (sa != sb) return pa == pb;
-  const long long d = ((pb - pa) % sa + sa) % sa;                              // where b's rows begin between the beginnings of a's
-  return d < ra || sa - d < rb;
-}
-// Whether the bytes of an array lie in a cache's pools, or the pools in one another.
-bool ranges_overlap(const void* a, long long na, const void* b, long long nb) {
-  const intptr_t pa = reinterpret_cast<intptr_t>(a), pb = reinterpret_cast<intptr_t>(b);
-  return a && b && pa < pb + nb && pb < pa + na;
-}
-struct Pools {
-  const void* at[4];
-  long long bytes[4];
-  explicit Pools(const rt_paged_cache* c) : at{c->k, c->v, c->k_exp, c->v_exp} {
-    const long long heads_rows = (long long)c->n_pages * c->n_kv_heads * c->page_size;
-    bytes[0] = bytes[1] = heads_rows * c->head_dim * (c->dtype == RT_E4M3 ? 1 : esize(c->dtype));
-    bytes[2] = bytes[3] = heads_rows;
+// The bytes of an array: n rows, one every `stride` bytes (a whole array is one row).  Rows without a pointer are nowhere.
+struct Bytes {
+  intptr_t at = 0;
+  long long row = 0, stride = 0, n = 0;
+  Bytes() = default;
+  Bytes(const void* p, long long bytes) : at(reinterpret_cast<intptr_t>(p)), row(bytes), stride(bytes), n(p && bytes > 0 ? 1 : 0) {}
+  Bytes(const void* p, int dtype, long long stride_, long long row_, long long rows) : Bytes(p, row_ * esize(dtype)) {
+    if (!n || rows <= 1 || stride_ == row_) { row *= rows; stride = row; n = p && row > 0 ? 1 : 0; }
+    else { stride = stride_ * esize(dtype); n = rows; }
   }
-  bool meet(const void* p, long long n, int first = 0) const {
-    for (int i = first; i < 4; ++i) if (ranges_overlap(p, n, at[i], bytes[i])) return true;
-    return false;
+  bool operator==(const Bytes& b) const { return at == b.at && row == b.row && stride == b.stride && n == b.n; }
+  intptr_t end() const { return at + (n - 1) * stride + row; }
+  bool meets(intptr_t from, intptr_t to) const {                               // whether a row shares bytes with [from, to)
+    const long long i = from < at + row ? 0 : (from - at - row) / stride + 1;  // the first row that ends behind `from`
+    return i < n && at + i * stride < to;
   }
-  bool meet_each_other() const { return meet(at[0], bytes[0], 1) || meet(at[1], bytes[1], 2) || meet(at[2], bytes[2], 3); }
 };
-long long extent(int dtype, long long stride, long long row, long long rows) { return ((rows - 1) * (rows > 1 ? stride : 0) + row) * esize(dtype); }
-bool same_rows(const void* a, long long stride_a, const void* b, long long stride_b, long long rows) { return a == b && (rows <= 1 || stride_a == stride_b); }
+// Whether two arrays share bytes.  Rows of one stride may lie in turn in one array (queries, keys and values of a projection).
+bool overlap(const Bytes& a, const Bytes& b) {
+  if (!a.n || !b.n || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.n == 1) return b.meets(a.at, a.end());
+  if (b.n == 1) return a.meets(b.at, b.end());
+  if (a.stride == b.stride) {
+    const long long d = ((b.at - a.at) % a.stride + a.stride) % a.stride;      // where b's rows begin between the beginnings of a's
+    return d < a.row || a.stride - d < b.row;
+  }
+  // rows of two strides in one stretch of memory: most such calls end with the first
+  for (long long i = b.at < a.at + a.row ? 0 : (b.at - a.at - a.row) / a.stride + 1; i < a.n && a.at + i * a.stride < b.end(); ++i)
+    if (b.meets(a.at + i * a.stride, a.at + i * a.stride + a.row)) return true;
+  return false;
+}
+// Whether one of the arrays that a call writes lies on another one, or on one that it reads.
+template <size_t N, size_t M>
+bool outputs_meet(const Bytes (&outs)[N], const Bytes (&ins)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t j = 0; j < i; ++j) if (overlap(outs[i], outs[j])) return true;
+    for (const Bytes& in : ins) if (overlap(outs[i], in)) return true;
+  }
+  return false;
+}
+// an input that an output may replace in its place
+Bytes unless(const Bytes& in, const Bytes& out) { return in == out ? Bytes() : in; }
+
+struct Pools {
+  Bytes k, v, k_exp, v_exp, table, status;
+  explicit Pools(const rt_paged_cache* c) : table(c->page_table, 4LL * c->n_seqs * c->max_pages), status(c->status, 4) {
+    const long long head_rows = (long long)c->n_pages * c->n_kv_heads * c->page_size, bytes = head_rows * c->head_dim * (c->dtype == RT_E4M3 ? 1 : esize(c->dtype));
+    k = Bytes(c->k, bytes); v = Bytes(c->v, bytes);
+    k_exp = Bytes(c->k_exp, head_rows); v_exp = Bytes(c->v_exp, head_rows);
+  }
+};
 
 // The pointer is memory of the current device (a pointer of another one would be a fault on the GPU, not an error).
 rt_status on_current_device(const void* p) {
@@ -131,8 +149,10 @@ rt_status rt_cache_write(const rt_paged_cache* cache, int32_t dtype, const void*
   rt_status st = cache_rows(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, &p);
   if (st != RT_OK || rows == 0) return st;
   const long long row = (long long)cache->n_kv_heads * cache->head_dim;
-  const Pools pools(cache);
-  if (pools.meet_each_other() || pools.meet(k, extent(dtype, k_stride, row, rows)) || pools.meet(v, extent(dtype, v_stride, row, rows))) return RT_ERR_INVALID_ARG;
+  const Pools to(cache);
+  const Bytes outs[] = {to.k, to.v, to.k_exp, to.v_exp};
+  const Bytes ins[] = {Bytes(k, dtype, k_stride, row, rows), Bytes(v, dtype, v_stride, row, rows), Bytes(seq, 4LL * rows), Bytes(pos, 4LL * rows), to.table, to.status};
+  if (outputs_meet(outs, ins)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   p.k_in = k; p.v_in = v;
   return cache_write_launch(dtype, p, (cudaStream_t)cuda_stream) == cudaSuccess ? RT_OK : RT_ERR_CUDA;
@@ -144,10 +164,10 @@ rt_status rt_cache_read(const rt_paged_cache* cache, int32_t dtype, void* k, voi
   rt_status st = cache_rows(cache, dtype, k, v, k_stride, v_stride, seq, pos, rows, &p);
   if (st != RT_OK || rows == 0) return st;
   const long long row = (long long)cache->n_kv_heads * cache->head_dim;
-  const Pools pools(cache);
-  if (rows_overlap(k, dtype, k_stride, row, v, dtype, v_stride, row, rows) || pools.meet(k, extent(dtype, k_stride, row, rows)) ||
-      pools.meet(v, extent(dtype, v_stride, row, rows)))
-    return RT_ERR_INVALID_ARG;
+  const Pools from(cache);
+  const Bytes outs[] = {Bytes(k, dtype, k_stride, row, rows), Bytes(v, dtype, v_stride, row, rows)};
+  const Bytes ins[] = {from.k, from.v, from.k_exp, from.v_exp, from.table, from.status, Bytes(seq, 4LL * rows), Bytes(pos, 4LL * rows)};
+  if (outputs_meet(outs, ins)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   p.k_out = k; p.v_out = v;
   return cache_read_launch(dtype, p, (cudaStream_t)cuda_stream) == cudaSuccess ? RT_OK : RT_ERR_CUDA;
@@ -170,13 +190,15 @@ rt_status rt_paged_attention(const rt_paged_cache* cache, const rt_paged_query* 
   if (q->k_own && (!rows_ok(q->k_own, q->dtype, q->k_own_stride, kv_row, B) || !rows_ok(q->v_own, q->dtype, q->v_own_stride, kv_row, B)))
     return RT_ERR_INVALID_ARG;
   if (q->n_heads / cache->n_kv_heads > 1024 || !paged_attn_counts(cache, q->n_heads)) return RT_ERR_UNSUPPORTED;
-  if (rows_overlap(q->out, q->dtype, q->out_stride, row, q->q, q->dtype, q->q_stride, row, B) ||
-      (q->k_own && (rows_overlap(q->out, q->dtype, q->out_stride, row, q->k_own, q->dtype, q->k_own_stride, kv_row, B) ||
-                    rows_overlap(q->out, q->dtype, q->out_stride, row, q->v_own, q->dtype, q->v_own_stride, kv_row, B))))
-    return RT_ERR_INVALID_ARG;
-  if (workspace_bytes < paged_attn_workspace(cache, q->n_heads)) return RT_ERR_WORKSPACE;
-  const Pools pools(cache);
-  if (pools.meet(q->out, extent(q->dtype, q->out_stride, row, B)) || pools.meet(q->lse, 4 * B * q->n_heads)) return RT_ERR_INVALID_ARG;
+  const Pools from(cache);
+  const Bytes out(q->out, q->dtype, q->out_stride, row, B), lse(q->lse, 4 * B * q->n_heads);
+  const Bytes ins[] = {Bytes(q->q, q->dtype, q->q_stride, row, B), Bytes(q->k_own, q->dtype, q->k_own_stride, kv_row, B), Bytes(q->v_own, q->dtype, q->v_own_stride, kv_row, B),
+                       Bytes(q->lens, 4 * B), Bytes(q->alibi_slopes, 4LL * q->n_heads), from.k, from.v, from.k_exp, from.v_exp, from.table, from.status};
+  for (int i = 0; i < 3; ++i) if (overlap(out, ins[i])) return RT_ERR_INVALID_ARG;
+  const size_t need = paged_attn_workspace(cache, q->n_heads);
+  if (workspace_bytes < need) return RT_ERR_WORKSPACE;
+  const Bytes outs[] = {out, lse, Bytes(workspace, (long long)need)};
+  if (outputs_meet(outs, ins)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(cache->k)) != RT_OK) return st;
   PagedAttnParams p;
   memset(&p, 0, sizeof(p));
@@ -199,11 +221,10 @@ rt_status rt_qk_rotate(const rt_rotate_config* cfg, const void* q, const void* k
     return RT_ERR_INVALID_ARG;
   if (rows == 0) return RT_OK;
   const int t = cfg->dtype;
-  if (!same_rows(q, q_stride, q_out, q_out_stride, rows) && rows_overlap(q, t, q_stride, qrow, q_out, t, q_out_stride, qrow, rows)) return RT_ERR_INVALID_ARG;
-  if (krow && ((!same_rows(k, k_stride, k_out, k_out_stride, rows) && rows_overlap(k, t, k_stride, krow, k_out, t, k_out_stride, krow, rows)) ||
-               rows_overlap(q_out, t, q_out_stride, qrow, k_out, t, k_out_stride, krow, rows) || rows_overlap(q_out, t, q_out_stride, qrow, k, t, k_stride, krow, rows) ||
-               rows_overlap(k_out, t, k_out_stride, krow, q, t, q_stride, qrow, rows)))
-    return RT_ERR_INVALID_ARG;
+  const Bytes qi(q, t, q_stride, qrow, rows), qo(q_out, t, q_out_stride, qrow, rows), ki = krow ? Bytes(k, t, k_stride, krow, rows) : Bytes(),
+              ko = krow ? Bytes(k_out, t, k_out_stride, krow, rows) : Bytes();
+  const Bytes outs[] = {qo, ko}, ins[] = {Bytes(g_q, qrow * esize(t)), krow ? Bytes(g_k, krow * esize(t)) : Bytes(), Bytes(pos, 4LL * rows)};
+  if (outputs_meet(outs, ins) || overlap(qo, unless(qi, qo)) || overlap(ko, unless(ki, ko)) || overlap(qo, ki) || overlap(ko, qi)) return RT_ERR_INVALID_ARG;
   if ((st = on_current_device(q)) != RT_OK) return st;
   RotateParams p;
   rotate_fill(cfg, &p);
@@ -229,13 +250,20 @@ rt_status rt_qk_rotate_backward(const rt_rotate_config* cfg, const void* q, cons
   if (krow && (!rows_ok(k, cfg->dtype, k_stride, krow, rows) || !rows_ok(dk_out, RT_F32, krow, krow, rows) || !rows_ok(dk, RT_F32, krow, krow, rows) ||
                !aligned16(g_k) || !aligned16(dg_k)))
     return RT_ERR_INVALID_ARG;
-  auto clash = [&](const void* a, long long ra, const void* b, long long rb) { return rows_overlap(a, RT_F32, ra, ra, b, RT_F32, rb, rb, rows); };
-  if ((dq != dq_out && clash(dq, qrow, dq_out, qrow)) || rows_overlap(dq, RT_F32, qrow, qrow, q, cfg->dtype, q_stride, qrow, rows)) return RT_ERR_INVALID_ARG;
-  if (krow && ((dk != dk_out && clash(dk, krow, dk_out, krow)) || clash(dq, qrow, dk, krow) || clash(dq, qrow, dk_out, krow) || clash(dk, krow, dq_out, qrow) ||
-               rows_overlap(dk, RT_F32, krow, krow, k, cfg->dtype, k_stride, krow, rows) || rows_overlap(dq, RT_F32, qrow, qrow, k, cfg->dtype, k_stride, krow, rows) ||
-               rows_overlap(dk, RT_F32, krow, krow, q, cfg->dtype, q_stride, qrow, rows) || ranges_overlap(dg_q, 4 * qrow, dg_k, 4 * krow)))
+  const int t = cfg->dtype;
+  const Bytes dqo(dq_out, 4 * qrow * rows), dko = krow ? Bytes(dk_out, 4 * krow * rows) : Bytes(), dqi(dq, 4 * qrow * rows), dki = krow ? Bytes(dk, 4 * krow * rows) : Bytes();
+  const Bytes outs[] = {dqi, dki, Bytes(dg_q, 4 * qrow), krow ? Bytes(dg_k, 4 * krow) : Bytes()};
+  const Bytes ins[] = {Bytes(q, t, q_stride, qrow, rows), krow ? Bytes(k, t, k_stride, krow, rows) : Bytes(), Bytes(g_q, qrow * esize(t)),
+                       krow ? Bytes(g_k, krow * esize(t)) : Bytes(), Bytes(pos, 4LL * rows)};
+  if (outputs_meet(outs, ins) || overlap(dqi, unless(dqo, dqi)) || overlap(dki, unless(dko, dki)) || overlap(dqi, dko) || overlap(dki, dqo) || overlap(outs[2], dqo) ||
+      overlap(outs[2], dko) || overlap(outs[3], dqo) || overlap(outs[3], dko))
     return RT_ERR_INVALID_ARG;
-  if (workspace_bytes < rotate_backward_workspace(cfg->n_heads + cfg->n_kv_heads, cfg->head_dim, rows)) return RT_ERR_WORKSPACE;
+  const size_t need = rotate_backward_workspace(cfg->n_heads + cfg->n_kv_heads, cfg->head_dim, rows);
+  if (workspace_bytes < need) return RT_ERR_WORKSPACE;
+  if (dg_q || (krow && dg_k)) {                                                // (otherwise nothing is written there)
+    const Bytes ws[] = {Bytes(workspace, (long long)need)}, all[] = {outs[0], outs[1], outs[2], outs[3], ins[0], ins[1], ins[2], ins[3], ins[4], dqo, dko};
+    if (outputs_meet(ws, all)) return RT_ERR_INVALID_ARG;
+  }
   if ((st = on_current_device(workspace)) != RT_OK) return st;
   RotateParams p;
   rotate_fill(cfg, &p);

@@ -123,3 +123,92 @@ def test_outputs_that_lie_in_the_pools_or_on_inputs_of_the_other_kind():
     call = lambda **kw: rt.rt_qk_rotate_backward(config(), *{**grad, **kw}.values(), None)
     for kw in (dict(dq=ADDR + big), dict(dk=ADDR), dict(dgq=ADDR + 6 * big, dgk=ADDR + 6 * big), dict(dgq=ADDR + 6 * big, dgk=ADDR + 6 * big + 256)):
         assert call(**kw) == BAD, kw
+
+
+def places(n):
+    """n addresses with 16 MB between them (nothing is read through them)."""
+    return [ADDR + (i << 24) for i in range(n)]
+
+
+def on_the_host(status):
+    """What a call with addresses of nothing ends with once its arguments have passed: there is no device here (and with one, no such memory)."""
+    import torch
+    return status == (BAD if torch.cuda.is_available() else rt.RT_ERR_CUDA)
+
+
+def test_attention_outputs_on_anything_else():
+    k, v, table, status, ke, ve, q, ko, vo, lens, slopes, out, lse, ws, free = places(15)
+    names = dict(q=q, k_own=ko, v_own=vo, lens=lens, alibi_slopes=slopes, out=out, lse=lse)
+    for f8 in (False, True):
+        c = rt.RtPagedCache(k, v, ke if f8 else None, ve if f8 else None, table, status, 8, 16, 2, 64, rt.RT_E4M3 if f8 else rt.RT_BF16, 3, 4)
+        need = rt.rt_paged_attention_workspace_bytes(c, 4)
+        call = lambda work=ws, **kw: rt.rt_paged_attention(c, rt.RtPagedQuery(*{**names, **kw}.values(), 256, 128, 128, 256, rt.RT_BF16, 4, 0.125), work, need, None)
+        assert on_the_host(call()) and on_the_host(call(lse=None, alibi_slopes=None)) and on_the_host(call(out=free)) and on_the_host(call(work=free, lse=ws))
+        pool = 8 * 2 * 16 * 64 * (1 if f8 else 2)
+        sizes = dict(k=(k, pool), v=(v, pool), table=(table, 48), status=(status, 4), q=(q, 3 * 512), k_own=(ko, 3 * 256), v_own=(vo, 3 * 256), lens=(lens, 12), slopes=(slopes, 16))
+        if f8:
+            sizes.update(k_exp=(ke, 256), v_exp=(ve, 256))
+        for name, (at, n) in sizes.items():
+            for there in (at, (at + n - 1) & ~15):                       # its first and its last 16 bytes
+                assert call(out=there) == BAD and call(lse=there) == BAD and call(work=there) == BAD, name
+            assert call(out=at - 3 * 512 + 16) == BAD and call(lse=at - 44) == BAD and call(work=at - need + 16) == BAD, name      # (its own last 16 bytes, the last number)
+            assert on_the_host(call(out=at - 3 * 512)) and on_the_host(call(lse=at - 48)) and on_the_host(call(work=at - need)), name
+            assert on_the_host(call(out=at + (n + 15) // 16 * 16)) and on_the_host(call(lse=at + (n + 3) // 4 * 4)), name
+        assert call(lse=out + 512) == BAD and call(work=out) == BAD and call(work=lse) == BAD
+
+
+def test_row_outputs_on_indexes_and_tables():
+    k, v, table, status, kr, vr, seq, pos, free = places(9)
+    c = rt.RtPagedCache(k, v, None, None, table, status, 8, 16, 2, 64, rt.RT_BF16, 3, 4)
+    names = dict(k=kr, v=vr, seq=seq, pos=pos)
+    for f in (rt.rt_cache_write, rt.rt_cache_read):
+        call = lambda c=c, ks=128, vs=128, **kw: f(c, rt.RT_BF16, *list({**names, **kw}.values())[:2], ks, vs, *list({**names, **kw}.values())[2:], 40, None)
+        assert on_the_host(call()) and on_the_host(call(k=kr, v=kr + 256, ks=256, vs=256))
+    read = lambda **kw: rt.rt_cache_read(c, rt.RT_BF16, *{**dict(k=kr, v=vr, ks=128, vs=128, seq=seq, pos=pos), **kw}.values(), 40, None)
+    for at in (seq, seq + 144, pos, table, table + 32, status):
+        assert read(k=at) == BAD and read(v=at) == BAD
+    # rows of two strides that lie in one stretch of memory: in the gaps, or on one another far from the beginning
+    assert on_the_host(read(k=kr, ks=512, v=kr + 256, vs=1024)) and on_the_host(read(k=kr, ks=1024, v=kr + 256, vs=512))
+    assert read(k=kr, ks=512, v=kr + 256, vs=136) == BAD and read(k=kr, ks=136, v=kr + 256, vs=512) == BAD
+    # rows of 256 bytes, 1280 and 1296 apart: the second ones begin 256 - 16 i bytes behind the first ones, or 256 + 16 i (and row 49 reaches row 50 of the others: 16 * 49 > 1280 - 512)
+    assert read(k=kr, ks=648, v=kr + 256, vs=640) == BAD and on_the_host(read(k=kr, ks=640, v=kr + 256, vs=648))
+    assert rt.rt_cache_read(c, rt.RT_BF16, kr, kr + 256, 640, 648, seq, pos, 51, None) == BAD and on_the_host(rt.rt_cache_read(c, rt.RT_BF16, kr, kr + 256, 640, 648, seq, pos, 50, None))
+    for kw in (dict(k=seq), dict(v=pos), dict(k=table), dict(v=table - 32752), dict(k=status), dict(k_exp=seq, v_exp=free, dtype=rt.RT_E4M3), dict(k_exp=free, v_exp=pos - 240, dtype=rt.RT_E4M3),
+               dict(k_exp=free, v_exp=table, dtype=rt.RT_E4M3)):
+        other = rt.RtPagedCache(k, v, None, None, table, status, 8, 16, 2, 64, rt.RT_BF16, 3, 4)
+        for n, x in kw.items():
+            setattr(other, n, x)
+        assert rt.rt_cache_write(other, rt.RT_BF16, kr, vr, 128, 128, seq, pos, 40, None) == BAD, kw
+
+
+def test_rotation_outputs_on_gains_and_positions():
+    q, k, gq, gk, pos, qo, ko, free = places(8)
+    base = dict(q=q, k=k, qs=256, ks=128, gq=gq, gk=gk, pos=pos, rows=40, qo=qo, ko=ko, qos=256, kos=128)
+    call = lambda cfg={}, **kw: rt.rt_qk_rotate(config(**cfg), *{**base, **kw}.values(), None)
+    assert on_the_host(call()) and on_the_host(call(qo=q, ko=k)) and on_the_host(call(qo=gk, ko=gk, cfg=dict(n_kv_heads=0)))
+    for at in (gq, gq + 496, gk, gk + 240, pos, pos + 144):
+        assert call(qo=at) == BAD and call(ko=at) == BAD
+    assert call(qo=q, qs=256, qos=264) == BAD and call(qo=q + 256, qs=264) == BAD and call(ko=k + 128 * 39, ks=136) == BAD
+    # rows of 512 bytes, 2048 apart: others in their gaps every 1024 or 4096 bytes, but not every 1536
+    assert on_the_host(call(q=q, qs=1024, qo=q + 512, qos=512)) and on_the_host(call(q=q, qs=1024, qo=q + 512, qos=2048)) and call(q=q, qs=1024, qo=q + 512, qos=768) == BAD
+
+
+def test_gradients_on_anything_else():
+    q, k, gq, gk, pos, dqo, dko, dq, dk, dgq, dgk, ws, free = places(13)
+    base = dict(q=q, k=k, qs=256, ks=128, gq=gq, gk=gk, pos=pos, rows=40, dqo=dqo, dko=dko, dq=dq, dk=dk, dgq=dgq, dgk=dgk, ws=ws)
+    need = rt.rt_qk_rotate_backward_workspace_bytes(config(), 40)
+    call = lambda cfg={}, **kw: rt.rt_qk_rotate_backward(config(**cfg), *{**base, **kw}.values(), need, None)
+    assert on_the_host(call()) and on_the_host(call(dq=dqo, dk=dko)) and on_the_host(call(dgq=None, dgk=None, ws=q)) and on_the_host(call(dgq=None))
+    sizes = dict(q=(q, 40 * 512), k=(k, 40 * 256), gq=(gq, 512), gk=(gk, 256), pos=(pos, 160), dqo=(dqo, 40 * 1024), dko=(dko, 40 * 512), dq=(dq, 40 * 1024), dk=(dk, 40 * 512),
+                 dgq=(dgq, 1024), dgk=(dgk, 512))
+    outs = dict(dq=40 * 1024, dk=40 * 512, dgq=1024, dgk=512, ws=need)
+    for out, n in outs.items():
+        for name, (at, size) in sizes.items():
+            if name == out:
+                continue
+            assert call(**{out: at + size - 16}) == BAD and call(**{out: at - n + 16}) == BAD, (out, name)
+            assert on_the_host(call(**{out: at + size})) and on_the_host(call(**{out: at - n // 16 * 16})), (out, name)
+            if (out, name) not in (("dq", "dqo"), ("dk", "dko")):
+                assert call(**{out: at}) == BAD, (out, name)
+    # without rows the gains' gradients are written all the same
+    assert call(rows=0, dgq=gq) == BAD and call(rows=0, dgq=free, dgk=free + 512) == BAD and on_the_host(call(rows=0, q=None, k=None, dqo=None, dko=None, dq=None, dk=None, pos=None))
