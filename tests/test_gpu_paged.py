@@ -952,3 +952,66 @@ def test_infinities_and_nan_stay_in_their_pair(shape, pairs, norm, dtype):
         s = size * gain.double().abs().view(x.shape[1:])
         same_numbers(dx, want, r * (s + u.abs() * (s * u.abs()).mean(-1, keepdim=True)) * (2 * hd + 64) * U)
         same_numbers(dg, (w * u).sum(0).reshape(-1), (size * u.abs()).sum(0).reshape(-1) * (R + hd + 64) * U)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("slack", [0, 40])
+def test_8_bit_pages_that_do_not_exist_and_lengths_that_are_cut(slack, hd, dtype):
+    # a unit of 64 positions has four pages of 16: any of them may be missing, in the middle and at the ragged end
+    rt = rt_module()
+    lens, H, kv = [70, 330, 64], 4, 2
+    c, ks, vs = make_cache(lens, kv, hd, 16, "e4m3", seed=16, slack=slack)
+    q = torch.randn((3, H, hd), generator=gen(4), device="cuda").to(TYPES[dtype])
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    lse = torch.empty((3, H), device="cuda")
+    check(c.attend(q, n, lse=lse), lse, reference(q, ks, vs, lens), dtype)
+    torch.cuda.synchronize()
+    assert c.status() == rt.RT_OK
+    for missing, bad in (([4], -1), ([5], c.k.shape[0]), ([6], 2 ** 31 - 1), ([7], -2 ** 31), ([8, 9, 10, 11], -1), ([20], -7), ([0, 3, 13], 1 << 30), (list(range(21)), -1)):
+        old = c.page_table[1].clone()
+        c.page_table[1, missing] = bad
+        out = c.attend(q, n, lse=lse)
+        torch.cuda.synchronize()
+        assert c.status() == rt.RT_ERR_INVALID_ARG
+        c.page_table[1] = old
+        c.clear_status()
+        keep = torch.tensor([j for j in range(330) if j // 16 not in missing], dtype=torch.long, device="cuda")
+        cut = lambda x: [x[0], x[1][keep], x[2]]                            # the pairs of those pages have no weight
+        check(out, lse, reference(q, cut(ks), cut(vs), lens), dtype)
+    if slack == 0:                                                        # a length beyond the table is cut to it: 336 positions, the last six written here
+        pos = torch.arange(330, 336, dtype=torch.int32, device="cuda")
+        x = torch.randn((6, kv, hd), generator=gen(8), device="cuda")
+        c.write(x, x, torch.ones_like(pos), pos)
+        x = c.read(torch.ones_like(pos), pos, dtype="f32")[0].double()
+        out = c.attend(q, torch.tensor([70, 2 ** 31 - 1, 64], dtype=torch.int32, device="cuda"), lse=lse)
+        torch.cuda.synchronize()
+        assert c.status() == rt.RT_ERR_INVALID_ARG
+        check(out, lse, reference(q, [ks[0], torch.cat((ks[1], x)), ks[2]], [vs[0], torch.cat((vs[1], x)), vs[2]], lens), dtype)
+
+
+@pytest.mark.parametrize("cache,dtype", [("e4m3", "bf16"), ("e4m3", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("hd,slack", [(64, 0), (64, 4000), (128, 0), (128, 4000)])
+def test_a_nan_that_is_attended_to_stays_in_its_head(hd, slack, cache, dtype):
+    # such heads are evaluated position by position: their other dimensions, and all other heads, are as good as ever
+    lens, H, kv = [300, 41, 700, 90], 6, 3
+    c, ks, vs = make_cache(lens, kv, hd, 16, cache, seed=18, slack=slack)
+    raw = lambda pool: pool.view(torch.uint8) if cache == "e4m3" else pool
+    nan = 0x7f if cache == "e4m3" else math.nan
+    place = lambda b, j: (int(c.page_table[b, j // 16]), j % 16)
+    marks = [(0, 1, 130, 5, "k"), (1, 0, 40, 9, "v"), (2, 2, 699, hd - 1, "v"), (2, 0, 3, 0, "v"), (3, 1, 0, 1, "k")]
+    for b, h, j, d, which in marks:
+        p, o = place(b, j)
+        raw(c.k if which == "k" else c.v)[p, h, o, d] = nan
+        (ks if which == "k" else vs)[b][j, h, d] = math.nan
+    q = torch.randn((4, H, hd), generator=gen(4), device="cuda").to(TYPES[dtype])
+    lse = torch.empty((4, H), device="cuda")
+    out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), lse=lse)
+    o, l, eo, el = reference(q, ks, vs, lens)
+    assert torch.equal(torch.isnan(out.float()), torch.isnan(o)) and torch.equal(torch.isnan(lse), torch.isnan(l))
+    assert int(torch.isnan(o).all(-1).sum()) == 4 and int(torch.isnan(o).sum()) == 4 * hd + 6        # two query heads on each head of the cache
+    # (the bound of a NaN dimension is NaN: nothing to compare there; the bounds of finite ones come from finite values)
+    fine = ~torch.isnan(o)
+    bound = HALF_STEP[dtype] * (o.abs() + eo) + eo + 1e-30
+    assert ((out.double() - o).abs() <= bound)[fine].all()
+    assert ((lse.double() - l).abs() <= el)[~torch.isnan(l)].all()
