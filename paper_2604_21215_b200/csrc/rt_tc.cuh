@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 
 #include "rt_common.cuh"
+#include "rt_known.h"
 
 namespace rt {
 
@@ -184,21 +185,18 @@ inline bool tensor_map_rows_bf16(CUtensorMap* out, const void* base, long long r
 // kernel and not to the thread that sets it, so it always becomes all that the device has beside the kernel's static arrays: a limit fitted to one
 // launch would take the shared memory from a wider launch of the same kernel by another thread.
 inline cudaError_t ensure_dynamic_smem(const void* fn, int bytes) {
-  struct Entry { const void* fn; int dev, bytes; };
-  constexpr int kEntries = 64;
-  thread_local Entry tab[kEntries];
-  thread_local int used = 0;
+  thread_local KnownKernels known;
   int dev = 0, most = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  for (int i = 0; i < used; ++i)
-    if (tab[i].fn == fn && tab[i].dev == dev) return bytes <= tab[i].bytes ? cudaSuccess : cudaErrorInvalidValue;
+  KnownKernels::Entry* entry = known.at(fn, dev);
+  if (entry->fn) return bytes <= entry->bytes ? cudaSuccess : cudaErrorInvalidValue;
   cudaFuncAttributes attr;
   if ((e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev)) != cudaSuccess || (e = cudaFuncGetAttributes(&attr, fn)) != cudaSuccess) return e;
   most -= (int)attr.sharedSizeBytes;
   if (bytes > most) return cudaErrorInvalidValue;
   e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-  if (e == cudaSuccess && used < kEntries) { tab[used].fn = fn; tab[used].dev = dev; tab[used].bytes = most; ++used; }
+  if (e == cudaSuccess) known.put(entry, fn, dev, most);
   return e;
 }
 
