@@ -307,8 +307,9 @@ rt_status rt_cache_read(const rt_paged_cache *cache, int32_t dtype, void *k, voi
  *   a_j = softmax_scale <q, k_j> - alibi_slopes[h] (p - j),  p = lens[b] with an own pair (at distance 0), else lens[b] - 1
  *   out = sum_j e^{a_j} v_j / sum_j e^{a_j},   lse = log sum_j e^{a_j}
  * A sequence without any pair gets out = 0 and lse = -infinity.  All arithmetic is fp32 or as good: softmax statistics and
- * sums in fp32, queries to 2^-22 of a row's largest, weights to 2^-20 (RT_E4M3: and to 2^-40 of the largest weight times
- * value scale).  `out` is rounded once.
+ * sums in fp32, queries to 2^-22 of a row's largest, weights to 2^-20 (RT_E4M3: and to 2^-39 of the largest weight times
+ * value scale).  Values times weights are added up by the tensor core for 16 positions (bf16 queries over bf16 pages of heads of 64: 32), which may cut a few
+ * 2^-23 of such a sum, and in fp32 from there on.  `out` is rounded once.
  * The work is split evenly over the GPU whatever the lengths are; the result does not depend on timing. */
 typedef struct {
   const void *q;                   /* [n_seqs, n_heads, head_dim] of `dtype` */
@@ -330,7 +331,8 @@ rt_status rt_paged_attention(const rt_paged_cache *cache, const rt_paged_query *
  *   y = x / sqrt(mean(x^2) + rms_eps) * g          (with norm_flags = RT_NORM_QK; otherwise y = x)
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),   t = pos[r] * freq[i],  i < rot_dim / 2
  * with (a, b) = (i, i + rot_dim / 2) for RT_PAIRS_HALVES and (2 i, 2 i + 1) for RT_PAIRS_NEIGHBOURS; dimensions from rot_dim on are
- * not rotated.  Turns are multiplied in 64 bits; sine and cosine are fp32's, with RT_BF16 to 2^-21.  q_out may be q and k_out may be k (with the same stride). */
+ * not rotated.  Squares are added up in fp32.  Angles are as good as pos * freq in 64-bit floating point (2^-53 of the product); sine and cosine are fp32's,
+ * with RT_BF16 to 2^-20.  q_out may be q and k_out may be k (with the same stride). */
 enum { RT_PAIRS_HALVES = 0, RT_PAIRS_NEIGHBOURS = 1 };
 typedef struct {
   int32_t dtype;                   /* RT_F32 or RT_BF16: queries, keys, gains and their outputs */

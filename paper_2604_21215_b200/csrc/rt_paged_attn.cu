@@ -1,10 +1,12 @@
 // Attention of one new token of every sequence over its cached pairs, in pages.
 //
 // Bound: HBM reads of the cached pairs (each is used once per head that shares it: one flop a byte for bf16, two for e4m3), if a unit costs few enough instructions
-// (e4m3: about 840 for 64 positions of a head of 64) and warps enough are there to hide its chain of products, maximum, exponentials and products.
-// Measured on one B200, of 6.55 TB/s: 16 sequences of 12 to 33 thousand pairs, 16 heads, e4m3 128 us (93 %); 128 of 1000, bf16 87 us (94 %);
-// 40 of 0.5 to 8 thousand, 16 query heads on 4 heads of 128, bf16 67 us (85 %); 24 of 0 to 4096, 12 heads 32.5 us (74 %: some 7 us of every call are launches, the first
-// trips to memory and the join; one sequence of 1024 takes 7.3 us).
+// (e4m3: about 890 for 64 positions of a head of 64) and warps enough are there to hide its chain of products, maximum, exponentials and products.
+// Measured on one B200, of 6.55 TB/s, in short runs of calls (SM clock 1.97 GHz): 16 sequences of 12 to 33 thousand pairs, 16 heads, e4m3 138 us (86 %; over seconds the
+// power cap takes the clock to 1.7 GHz, and it is 163); 128 of 1000, bf16 87 us (93 %); 40 of 0.5 to 8 thousand, 16 query heads on 4 heads of 128, bf16 67.5 us (84 %); 24 of 0 to
+// 4096, 12 heads 33.2 us (72 %: some 7 us of every call are launches, the first trips to memory and the join; one sequence of 1024 takes 7.3 us).
+// Far from that: heads that are cut by many warps (173 of 1 to 476, 12 heads, e4m3 32 %), e4m3 heads of 128 in middling calls (30 of 1647 51 %), fp32 pages with shared
+// heads (39 to 56 %: a shuffle for every weight), more than 8 query heads on one (54 %: the pairs are read for each 8).
 //
 // Split.  The work of a call is a line of units: sequence by sequence, head of the cache by head, KT positions a unit.  Every warp of the
 // launch takes an equal piece of that line, wherever it begins and ends, so one long sequence among short ones costs no more than its bytes;
@@ -19,7 +21,7 @@
 // Products.  One query row cannot fill a tensor-core tile, but a tile is the cheapest way to use a staged row for all heads that share it:
 // up to 8 query heads are rows 0-7 of the A operand of mma m16n8k16 (registers on both sides: with one row of 16 in use and operands read once, tcgen05's
 // shared-memory operands and its accumulators' way through TMEM would cost more than the products).  Rows 8-15 carry the second term of the same heads' fp32 numbers, split
-// into 16-bit terms; so scores and weights keep at least 22 bits.  Positions and dimensions are permuted so that each operand is one 16-byte load of a
+// into 16-bit terms, together 22 bits or more (weights are good to 2^-20, with exp2 and the rounding of its argument).  Positions and dimensions are permuted so that each operand is one 16-byte load of a
 // row (an order of the contraction is free, and so is the order of the output's columns as long as the epilogue knows it): no transposition.
 //   bf16 pages: bf16 products, queries in 1 (bf16) or 3 terms (fp32), weights in 3 terms.
 //   e4m3 pages: codes are exact in fp16; fp16 products, queries (scaled by a power of two) in 1 or 2 terms, weights in 2 terms.  The keys' scales
@@ -37,7 +39,7 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 8;      // warps of a block; query heads of a unit
 constexpr int kSms = 148;
-constexpr float kWeightLog2 = 15.0f, kWeightBack = 1.0f / 32768.0f;      // fp16 weights lie in [0, 2^15]: their two terms keep 2^-40 of the largest
+constexpr float kWeightLog2 = 15.0f, kWeightBack = 1.0f / 32768.0f;      // fp16 weights lie in [0, 2^15], the largest above 2^14: their two terms keep 2^-39 of it
 
 // ---- shapes ------------------------------------------------------------------------------------
 template <typename CT, int HD>
@@ -51,7 +53,7 @@ struct Shape {
   static constexpr int STAGE = ((KV + EXP > OUT ? KV + EXP : OUT) + 127) / 128 * 128;
   // Units of a ring, and blocks of an SM (both limited by the SM's 227 KB, and by 65,536 registers).  Twelve warps an SM with two units of 8 KB hide a unit's chain
   // better than eight with three (ragged bf16 batch 32.5 us against 37.9) or twelve and sixteen with units of 4 KB (34.9, 33.1); e4m3 units of 64 positions instead of 32
-  // spread what a unit costs besides its products (128 us against 143).  Heads of 128 in bf16 need the registers of eight warps.
+  // spread what a unit costs besides its products (128 us against 143, both with sums in the tensor core).  Heads of 128 in bf16 need the registers of eight warps.
   static constexpr bool SMALL = HD == 64 && sizeof(CT) <= 2;
   static constexpr int STAGES = KV <= 4096 ? 4 : SMALL ? 2 : 3;
   static constexpr int CTAS = KV <= 4096 || SMALL ? 3 : KV <= 8192 ? 2 : 1;

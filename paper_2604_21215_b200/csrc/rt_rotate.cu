@@ -4,8 +4,9 @@
 // two loads of 4 elements, so the rotation needs no exchange and the norm a few shuffles.  Dimensions that are not rotated make pairs too, which stay as
 // they are.  A warp takes the heads of one row side by side: its lanes form the row's angles once, one or two each.  All products are paired fp32
 // instructions.
-// Measured on one B200, of 6.55 TB/s: 8 x 4050 rows of 16 + 16 heads of 64 with gains, bf16 44 us (92 %), fp32 89 %; 8 + 8 heads of 128 93 %, 16 + 4 of 64 89 %, 16 + 4 of 128 84 %,
-// 4 + 4 of 64 57 % in bf16 (angles and addresses of a short row), 100 % in fp32.  Gradients 111 us (91 %), 8 + 8 heads of 128 113 us (90 %), 16 + 4 of 128 92 %.
+// Measured on one B200, of 6.55 TB/s, in a run of calls: 8 x 4050 rows of 16 + 16 heads of 64 with gains, bf16 44.6 us (91 %); 30000 rows: fp32 89 %, 8 + 8 heads of 128 89 %, 16 + 4 of
+// 64 77 %, 16 + 4 of 128 83 %, 4 + 4 of 64 60 % and 3 + 3 46 % in bf16 (angles and addresses of a short row), 4 + 4 in fp32 100 %.  Gradients of 8 x 4050 rows 112 us (90 %); 30000 rows of
+// 8 + 8 heads of 128 104 us (90 %), 16 + 4 of 128 89 %; 12000 rows of 4 + 1 heads of 128 54 %.
 #include "rt_paged.h"
 #include "rt_tc.cuh"
 
@@ -141,8 +142,9 @@ struct Turn {
 };
 
 // Pair n's angle is formed by lane n % 32 of the warp and handed to the lanes that hold the pair through 512 bytes of shared memory of the warp's own (two loads a lane,
-// where shuffles would be 8 or 16).  Turns are multiplied as 64-bit fractions, whole turns falling off at the top: far positions keep their angles (2^-34 turns from
-// the rounding of a turn, 2^-33 from that of the product to 32 bits, 2^-24 of itself in fp32), and it takes two integer products where fp64 would take six slow instructions.
+// where shuffles would be 8 or 16).  Turns are multiplied as 64-bit fractions, whole turns falling off at the top: far positions keep their angles (the turns of one position
+// come from fp64, so they are off by 2^-53 of all that has been turned, as a product in fp64 would be; 2^-33 turns from the rounding to 32 bits, 2^-24 of itself in fp32), and it
+// takes two integer products where fp64 would take six slow instructions.
 struct Angles { float cos[64], sin[64]; };
 template <int LPR> struct Turns {                                      // of this lane's pairs
   unsigned long long per[LPR / 8];
@@ -150,7 +152,7 @@ template <int LPR> struct Turns {                                      // of thi
 #pragma unroll
     for (int k = 0; k < LPR / 8; ++k) per[k] = p.turns[lane + 32 * k];      // (zero where there is no pair)
   }
-  // EXACT: to fp32's rounding; otherwise to 2^-21, for rows that are rounded to bf16 (2^-9)
+  // EXACT: to fp32's rounding; otherwise to 2^-20, for rows that are rounded to bf16 (2^-9): 2^-21.2 of __cosf and 2^-21.7 of an angle near a half turn in fp32
   template <bool EXACT>
   __device__ __forceinline__ void make(int pos, int lane, Angles& buf) const {
 #pragma unroll
